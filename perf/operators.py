@@ -173,7 +173,7 @@ def prepare(case, seed):
     logits = torch.zeros((B, T, ld), dtype=dt, device="cuda")[:, :, :V]
     tokens = torch.zeros((B, T), dtype=torch.int32, device="cuda")
     state = dict(case=case, logits=logits, tokens=tokens, window=_int32(window),
-                 rollout=_int32(rollout), rows=_row_list(ends))
+                 rollout=_int32(rollout), rows=_row_list(ends), status=_int32([0]))
     path = case["path"]
     with_list = K > 0 and path != "logprobs"
     if with_list:
@@ -229,7 +229,7 @@ def _prepare_linear(case, seed):
         wq[v0:v0 + w.shape[0], :d] = q.to(torch.int8)
         w_scale[v0:v0 + w.shape[0]] = s
     return dict(case=case, hidden=hidden, wq=wq[:, :d], w_scale=w_scale,
-                logits=torch.zeros((M, V), dtype=_DTYPES[case["out"]], device="cuda"))
+                logits=torch.zeros((M, V), dtype=_DTYPES[case["out"]], device="cuda"), status=_int32([0]))
 
 
 def _row_list(ends):
@@ -260,7 +260,8 @@ def run(state):
 def _own_logprobs(s):
     from paper_2605_28396_b200 import api
     o = api.adwin_token_logprobs(s["logits"], s["tokens"], s["window"], s["rollout"],
-                                 top_k=s["case"]["K"], want_entropy=s["case"]["entropy"])
+                                 top_k=s["case"]["K"], want_entropy=s["case"]["entropy"],
+                                 dev_status=s["status"])
     return _scores(o.logprob, o.entropy, o.lse, o.top_ids, o.top_logprobs, o.rest)
 
 
@@ -269,7 +270,8 @@ def _own_grad(s):
     o = api.adwin_token_logprobs_bwd(s["logits"], s["tokens"], s["lse"], s["window"], s["rollout"],
                                      d_logprob=s["d_logprob"], d_entropy=s["d_entropy"],
                                      entropy=s["entropy"] if s["d_entropy"] is not None else None,
-                                     top_ids=s.get("top_ids"), d_top=s["d_top"], grad=s["grad"])
+                                     top_ids=s.get("top_ids"), d_top=s["d_top"], grad=s["grad"],
+                                     dev_status=s["status"])
     return dict(grad=o.grad)
 
 
@@ -279,14 +281,14 @@ def _own_topk_kl(s):
     o = api.adwin_opd_topk_kl_fwd_bwd(s["logits"], s["tokens"], s["top_ids"], s["top_logprobs"],
                                       s["window"], s["rollout"], rest=s["rest"] if c["rest"] else None,
                                       kl_mode=api.KL_FORWARD if c["mode"] == "forward" else api.KL_REVERSE,
-                                      grad=s["grad"], want_lse=True)
+                                      grad=s["grad"], want_lse=True, dev_status=s["status"])
     return dict(kl=o.kl, logratio=o.logratio, gsq=o.gsq, lse=o.lse_s, grad=o.grad)
 
 
 def _own_linear(s):
     from paper_2605_28396_b200 import api
-    q, scale = api.adwin_quantize_rows_i8(s["hidden"])
-    out = api.adwin_linear_i8(q, scale, s["wq"], s["w_scale"], out=s["logits"])
+    q, scale = api.adwin_quantize_rows_i8(s["hidden"], dev_status=s["status"])
+    out = api.adwin_linear_i8(q, scale, s["wq"], s["w_scale"], out=s["logits"], dev_status=s["status"])
     return dict(logits=out, scale=scale)
 
 
