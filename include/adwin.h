@@ -76,6 +76,14 @@ enum {
                               of it (a call that processes nothing, B = 0 or T = 0, leaves it alone) */
 };
 
+/* Which divergence adwin_opd_topk_kl_fwd_bwd evaluates. */
+typedef enum {
+  ADWIN_KL_REVERSE = 0, /* KL(student || teacher) over the alternatives and the rest */
+  ADWIN_KL_FORWARD = 1  /* KL(teacher || student) over the same */
+} adwin_kl_mode_t;
+
+enum { ADWIN_TOP_MAX = 128 }; /* longest list of alternatives */
+
 /* Flags returned by adwin_probe_align in *flags_out. */
 enum {
   ADWIN_ALIGN_DEGENERATE = 1,      /* some full-rollout squared norm was 0: that rho was set to 1 */
@@ -400,6 +408,61 @@ int adwin_opd_kl_fwd_bwd_no_alloc(const void* student_logits, const void* teache
                                   int flags, void* grad_student, int grad_dtype, int64_t ld_grad,
                                   float* kl, float* logratio, float* gsq, float* lse_student,
                                   float* lse_teacher, int32_t* dev_status, void* cuda_stream);
+
+/*
+ * Scores of given tokens under one policy, one read of the logits: what a teacher serves to the
+ * student it supervises, and what a policy-gradient loss needs of the policy itself.  For every
+ * position t < E_b = min(W_b, R_b, T), with p = softmax(z), z = logits[b,t,:]:
+ *   lse[b,t]      = log sum_k exp z_k
+ *   logprob[b,t]  = log p_y                       y = tokens[b,t]
+ *   entropy[b,t]  = -sum_k p_k log p_k            nats
+ *   top_ids[b,t,:], top_logprobs[b,t,:]           the K most likely entries in descending order and
+ *                                                 their log probabilities; equal logits in the
+ *                                                 order of their index
+ *   rest[b,t]     = log of the mass outside them  (-inf where there is none)
+ * Other positions get 0, in top_ids -1.  Sums are fp32; rest is summed over the entries outside the
+ * list, not taken from 1, so that it keeps its relative precision however small the mass is.
+ *
+ * logits       : [B,T,V], element type `dtype`, row stride ld >= V elements, any alignment
+ * tokens       : [B,T] int32;  window, rollout_len: [B] int32 or NULL (= T)
+ * K            : 0 <= K <= min(V, ADWIN_TOP_MAX); with K = 0 top_ids, top_logprobs, rest are ignored
+ * logprob      : [B,T] fp32.  entropy, lse, rest: [B,T] fp32 or NULL
+ * top_ids      : [B,T,K] int32.  top_logprobs: [B,T,K] fp32
+ * flags        : ADWIN_STATUS_INIT
+ * Entries of -inf and of the type's lowest value are masked entries like any others.  A row whose
+ * lse is not finite (nothing left, +inf, NaN) raises ADWIN_DEV_NONFINITE: its scores are NaN, its
+ * top_ids -1, its lse is what it is.  A token outside [0,V) gives logprob NaN and
+ * ADWIN_DEV_TOKEN_RANGE.  The paper's per-token reward and cost (Section 2.3, App. A.1) are
+ * differences of two such logprobs; entropy is that of adwin_teacher_drift (Section 3.1).
+ */
+int adwin_token_logprobs(const void* logits, int dtype, int64_t B, int64_t T, int64_t V, int64_t ld,
+                         const int32_t* tokens, const int32_t* window, const int32_t* rollout_len,
+                         int32_t K, int flags, float* logprob, float* entropy, float* lse,
+                         int32_t* top_ids, float* top_logprobs, float* rest, int32_t* dev_status,
+                         void* cuda_stream);
+
+/*
+ * Gradient of a loss of these scores with respect to the logits, for positions t < E_b:
+ *   grad_k = d_logprob (1[k=y] - p_k) - d_entropy p_k (log p_k + entropy)
+ *            + sum_j d_top_j (1[k=top_ids_j] - p_k),        p_k = exp(z_k - lse)
+ * lse, entropy as adwin_token_logprobs returned them; d_logprob, d_entropy [B,T], d_top [B,T,K]
+ * fp32: the loss's derivatives, each or NULL (= 0).  entropy may be NULL without d_entropy, top_ids
+ * without d_top (then K is ignored).  `rest` carries no gradient.  Entries of top_ids may repeat one another and
+ * the token; -1 stands for none.  Other indices outside [0,V) are left out and raise
+ * ADWIN_DEV_TOKEN_RANGE.  A row all of whose derivatives are 0 has the gradient 0, whatever its
+ * logits, which are not read.  lse is an fp32 number: where it is of size 1e6 and more (nothing left
+ * but entries masked by -1e30) it no longer tells p_k apart from its neighbours.
+ * grad         : [B,T,V] of grad_dtype, row stride ld_grad; rows t >= E_b are left as they are, or
+ *                zero-filled with ADWIN_ZERO_TAIL.  It may be the logits buffer itself (same pointer,
+ *                dtype and stride); any other overlap is not allowed
+ * flags        : ADWIN_ZERO_TAIL, ADWIN_STATUS_INIT
+ */
+int adwin_token_logprobs_bwd(const void* logits, int dtype, int64_t B, int64_t T, int64_t V,
+                             int64_t ld, const int32_t* tokens, const int32_t* window,
+                             const int32_t* rollout_len, const float* lse, const float* entropy,
+                             const float* d_logprob, const float* d_entropy, const int32_t* top_ids,
+                             const float* d_top, int32_t K, int flags, void* grad, int grad_dtype,
+                             int64_t ld_grad, int32_t* dev_status, void* cuda_stream);
 
 #ifdef __cplusplus
 }

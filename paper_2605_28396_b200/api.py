@@ -20,6 +20,8 @@ F32, BF16 = 0, 1
 GRAD_FULL_KL, GRAD_SAMPLED = 0, 1
 ZERO_TAIL, RANGE_FULL, FORCE_GENERIC, FORCE_STAGED, STATUS_INIT = 1, 2, 4, 8, 32
 DEV_TOKEN_RANGE, DEV_NONFINITE, DEV_TIMEOUT, DEV_BOUNDS, DEV_WINDOW, DEV_WORKSPACE = 1, 2, 4, 8, 16, 32
+KL_REVERSE, KL_FORWARD = 0, 1
+TOP_MAX = 128
 ALIGN_DEGENERATE, ALIGN_NONE_ADMISSIBLE = 1, 2
 DEFAULT_CANDIDATES = (64, 128, 256, 512, 1024, 2048)   # Section 5.1, Training Details
 RHO_STAR = math.sqrt(2.0) / 2.0                          # Section 4.2, threshold equation
@@ -31,7 +33,7 @@ EXPORTS = ("adwin_version", "adwin_status_string", "adwin_workspace_bytes",
            "adwin_return_to_go", "adwin_opd_kl_fwd_bwd_weighted", "adwin_teacher_drift",
            "adwin_drift_curves", "adwin_lmhead_workspace_bytes", "adwin_opd_kl_lmhead_fwd_bwd",
            "adwin_diag_set_wait_limit_ns", "adwin_lmhead_align_workspace_bytes",
-           "adwin_lmhead_weight_align")
+           "adwin_lmhead_weight_align", "adwin_token_logprobs", "adwin_token_logprobs_bwd")
 
 _lib = None
 
@@ -112,6 +114,13 @@ def lib():
         L.adwin_lmhead_weight_align.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, i64, vp, vp,
                                                 vp, i32, f64, ctypes.c_int, vp, vp, vp, vp, vp,
                                                 vp, i64, vp, sz, vp, vp]
+        L.adwin_token_logprobs.restype = ctypes.c_int
+        L.adwin_token_logprobs.argtypes = [vp, ctypes.c_int, i64, i64, i64, i64, vp, vp, vp, i32,
+                                           ctypes.c_int, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.adwin_token_logprobs_bwd.restype = ctypes.c_int
+        L.adwin_token_logprobs_bwd.argtypes = [vp, ctypes.c_int, i64, i64, i64, i64, vp, vp, vp, vp,
+                                               vp, vp, vp, vp, vp, i32, ctypes.c_int, vp,
+                                               ctypes.c_int, i64, vp, vp]
         L.adwin_diag_set_wait_limit_ns.restype = None
         L.adwin_diag_set_wait_limit_ns.argtypes = [ctypes.c_uint64]
         _lib = L
@@ -497,3 +506,114 @@ def adwin_lmhead_weight_align(hidden_student, w_student, hidden_teacher, w_teach
         workspace.numel() - off, _ptr(dev_status), _stream(dev)))
     return SimpleNamespace(batch_stats=stats, L_next=L_next, flags=flags, kl=kl, logratio=logratio,
                            gsq=gsq, dev_status=dev_status, candidates=cands, workspace=workspace)
+
+
+def _int32_arg(name, t, shape, device):
+    """An index or length array the kernels read: int32, contiguous, on the call's device."""
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or
+                          t.device != device):
+        raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {shape} on {device}")
+
+
+def _f32_arg(name, t, shape, device):
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape or
+                          not t.is_contiguous() or t.device != device):
+        raise ValueError(f"{name}: expected a contiguous float32 tensor of shape {shape} on {device}")
+
+
+def _logit_rows(x):
+    """Shape, device and row stride of [B,T,V] logits or of their gradient."""
+    if x.dim() != 3:
+        raise ValueError("logits and gradients are [B,T,V] tensors")
+    B, T, V = x.shape
+    sb, st, sv = x.stride()
+    ld = st if T > 1 else (sb if B > 1 else V)
+    if (V > 1 and sv != 1) or (B > 1 and T > 1 and sb != T * ld) or ld < V:
+        raise ValueError("the last dimension must be contiguous and rows at one uniform stride")
+    return B, T, V, ld
+
+
+def _own_status(dev_status, device, n_rows, flags):
+    if dev_status is None:
+        return _new_status(device, n_rows, flags)
+    _int32_arg("dev_status", dev_status, (1,), device)
+    return dev_status, flags
+
+
+def adwin_token_logprobs(logits, tokens, window=None, rollout_len=None, *, top_k=0,
+                         want_entropy=True, want_lse=True, flags=0, dev_status=None):
+    """Log probability of each given token, entropy, log-sum-exp and the top_k alternatives with
+    their log probabilities and the log of the mass outside them (see include/adwin.h).
+
+    logits: [B,T,V] CUDA tensor (fp32 or bf16), last dim contiguous, rows at a uniform stride.
+    window, rollout_len: [B] int32 or None (whole rollouts).  Returns a namespace with logprob,
+    entropy, lse [B,T] fp32, top_ids [B,T,top_k] int32, top_logprobs [B,T,top_k], rest [B,T] fp32
+    (None where not asked for) and dev_status.  A caller that passes its own status word collects
+    its bits there over calls; nothing is synchronised.
+    """
+    B, T, V, ld = _logit_rows(logits)
+    dev = logits.device
+    stream = _stream(dev)
+    _int32_arg("tokens", tokens, (B, T), dev)
+    _int32_arg("window", window, (B,), dev)
+    _int32_arg("rollout_len", rollout_len, (B,), dev)
+    K = int(top_k)
+    if not 0 <= K <= min(V, TOP_MAX):
+        raise ValueError(f"top_k must be between 0 and min(V, {TOP_MAX})")
+    dt = _dtype_code(logits.dtype)
+    dev_status, flags = _own_status(dev_status, dev, B * T, flags)
+    # one allocation for the scalars, one for the alternatives' scores
+    s = _scalars(1 + (1 if want_entropy else 0) + (1 if want_lse else 0) + (1 if K else 0), B, T, dev)
+    o = SimpleNamespace(logprob=s[0], entropy=s[1] if want_entropy else None,
+                        lse=s[2 if want_entropy else 1] if want_lse else None, top_ids=None,
+                        top_logprobs=None, rest=None, dev_status=dev_status)
+    if K:
+        o.rest = s[-1]
+        o.top_ids = torch.empty((B, T, K), dtype=torch.int32, device=dev)
+        o.top_logprobs = torch.empty((B, T, K), dtype=torch.float32, device=dev)
+    _check(lib().adwin_token_logprobs(
+        _ptr(logits), dt, B, T, V, ld, _ptr(tokens), _ptr(window), _ptr(rollout_len), K, int(flags),
+        _ptr(o.logprob), _ptr(o.entropy), _ptr(o.lse), _ptr(o.top_ids), _ptr(o.top_logprobs),
+        _ptr(o.rest), _ptr(dev_status), stream))
+    return o
+
+
+def adwin_token_logprobs_bwd(logits, tokens, lse, window=None, rollout_len=None, *, d_logprob=None,
+                             d_entropy=None, entropy=None, top_ids=None, d_top=None, grad=None,
+                             grad_dtype=None, flags=0, dev_status=None):
+    """Gradient with respect to the logits of a loss of ``adwin_token_logprobs``'s scores, from the
+    loss's derivatives d_logprob, d_entropy [B,T], d_top [B,T,K] (each or None; see include/adwin.h).
+
+    lse, entropy: as returned by the forward call.  ``grad``: a [B,T,V] tensor to write into (the
+    logits themselves are allowed), or None to have one of ``grad_dtype`` (the logits' by default)
+    allocated, uninitialised outside the windows unless ZERO_TAIL.  Returns a namespace with grad
+    and dev_status.
+    """
+    B, T, V, ld = _logit_rows(logits)
+    dev = logits.device
+    stream = _stream(dev)
+    _int32_arg("tokens", tokens, (B, T), dev)
+    _int32_arg("window", window, (B,), dev)
+    _int32_arg("rollout_len", rollout_len, (B,), dev)
+    for name, t in (("lse", lse), ("entropy", entropy), ("d_logprob", d_logprob),
+                    ("d_entropy", d_entropy)):
+        _f32_arg(name, t, (B, T), dev)
+    K = 0
+    if d_top is not None:
+        K = d_top.shape[-1]
+        _f32_arg("d_top", d_top, (B, T, K), dev)
+        _int32_arg("top_ids", top_ids, (B, T, K), dev)
+        if K == 0:
+            d_top = None
+    if grad is None:
+        grad = torch.empty((B, T, V), dtype=grad_dtype or logits.dtype, device=dev)
+    if tuple(grad.shape) != (B, T, V) or grad.device != dev:
+        raise ValueError("grad must have the logits' shape and device")
+    ld_grad = _logit_rows(grad)[3]
+    dt, gdt = _dtype_code(logits.dtype), _dtype_code(grad.dtype)
+    dev_status, flags = _own_status(dev_status, dev, B * T, flags)
+    _check(lib().adwin_token_logprobs_bwd(
+        _ptr(logits), dt, B, T, V, ld, _ptr(tokens), _ptr(window), _ptr(rollout_len), _ptr(lse),
+        _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _ptr(top_ids), _ptr(d_top), K, int(flags),
+        _ptr(grad), gdt, ld_grad, _ptr(dev_status), stream))
+    return SimpleNamespace(grad=grad, dev_status=dev_status)

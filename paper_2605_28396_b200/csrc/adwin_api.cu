@@ -37,6 +37,11 @@ int sm_count_of_current_device() {
   return cached[dev];
 }
 
+// ADWIN_STATUS_INIT for the calls without a row map, whose kernel would otherwise clear the word.
+bool status_init(int flags, int32_t* status, cudaStream_t s) {
+  return !(flags & ADWIN_STATUS_INIT) || cudaMemsetAsync(status, 0, sizeof(int32_t), s) == cudaSuccess;
+}
+
 }  // namespace
 }  // namespace adwin
 
@@ -153,6 +158,68 @@ int adwin_drift_curves(const float* entropy, const int32_t* rank, const int32_t*
     return ADWIN_ERR_ALIGN;
   if (launch_drift_curves(entropy, rank, rollout_len, B, T, ks, K, worst_rank, survival, bf_mean,
                           n_active, static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess)
+    return ADWIN_ERR_CUDA;
+  return ADWIN_OK;
+}
+
+int adwin_token_logprobs(const void* logits, int dtype, int64_t B, int64_t T, int64_t V, int64_t ld,
+                         const int32_t* tokens, const int32_t* window, const int32_t* rollout_len,
+                         int32_t K, int flags, float* logprob, float* entropy, float* lse,
+                         int32_t* top_ids, float* top_logprobs, float* rest, int32_t* dev_status,
+                         void* cuda_stream) {
+  if (dtype != ADWIN_F32 && dtype != ADWIN_BF16) return ADWIN_ERR_DTYPE;
+  if (flags & ~ADWIN_STATUS_INIT) return ADWIN_ERR_DTYPE;
+  if (B < 0 || T < 0 || B > kMaxB || T > kMaxT || V < 1 || V > kMaxV || ld < V || K < 0 || K > V ||
+      K > ADWIN_TOP_MAX)
+    return ADWIN_ERR_SHAPE;
+  if (!dev_status) return ADWIN_ERR_NULL;
+  if (B == 0 || T == 0) return ADWIN_OK;
+  if (!logits || !tokens || !logprob || (K > 0 && (!top_ids || !top_logprobs))) return ADWIN_ERR_NULL;
+  if (!aligned(logits, elem_size(dtype)) || !aligned(tokens, 4) || !aligned(window, 4) ||
+      !aligned(rollout_len, 4) || !aligned(logprob, 4) || !aligned(entropy, 4) || !aligned(lse, 4) ||
+      !aligned(dev_status, 4) ||
+      (K > 0 && (!aligned(top_ids, 4) || !aligned(top_logprobs, 4) || !aligned(rest, 4))))
+    return ADWIN_ERR_ALIGN;
+  const int sms = sm_count_of_current_device();
+  if (sms <= 0) return ADWIN_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (!status_init(flags, dev_status, s)) return ADWIN_ERR_CUDA;
+  if (launch_token_scores(logits, dtype, B, T, V, ld, tokens, window, rollout_len, K, logprob, entropy, lse,
+                          top_ids, top_logprobs, rest, dev_status, sms, s) != cudaSuccess)
+    return ADWIN_ERR_CUDA;
+  return ADWIN_OK;
+}
+
+int adwin_token_logprobs_bwd(const void* logits, int dtype, int64_t B, int64_t T, int64_t V,
+                             int64_t ld, const int32_t* tokens, const int32_t* window,
+                             const int32_t* rollout_len, const float* lse, const float* entropy,
+                             const float* d_logprob, const float* d_entropy, const int32_t* top_ids,
+                             const float* d_top, int32_t K, int flags, void* grad, int grad_dtype,
+                             int64_t ld_grad, int32_t* dev_status, void* cuda_stream) {
+  if (dtype != ADWIN_F32 && dtype != ADWIN_BF16) return ADWIN_ERR_DTYPE;
+  if (grad_dtype != ADWIN_F32 && grad_dtype != ADWIN_BF16) return ADWIN_ERR_DTYPE;
+  if (flags & ~(ADWIN_STATUS_INIT | ADWIN_ZERO_TAIL)) return ADWIN_ERR_DTYPE;
+  if (B < 0 || T < 0 || B > kMaxB || T > kMaxT || V < 1 || V > kMaxV || ld < V || ld_grad < V ||
+      (d_top && (K < 1 || K > ADWIN_TOP_MAX)))
+    return ADWIN_ERR_SHAPE;
+  if (!dev_status) return ADWIN_ERR_NULL;
+  if (B == 0 || T == 0) return ADWIN_OK;
+  if (!logits || !tokens || !lse || !grad || (d_entropy && !entropy) || (d_top && !top_ids))
+    return ADWIN_ERR_NULL;
+  if (!aligned(logits, elem_size(dtype)) || !aligned(grad, elem_size(grad_dtype)) || !aligned(tokens, 4) ||
+      !aligned(window, 4) || !aligned(rollout_len, 4) || !aligned(lse, 4) || !aligned(entropy, 4) ||
+      !aligned(d_logprob, 4) || !aligned(d_entropy, 4) || !aligned(dev_status, 4) ||
+      (d_top && (!aligned(top_ids, 4) || !aligned(d_top, 4))))
+    return ADWIN_ERR_ALIGN;
+  // in place: an entry's gradient takes the place of the logit it is formed from
+  if (grad == logits && (grad_dtype != dtype || ld_grad != ld)) return ADWIN_ERR_UNSUPPORTED;
+  const int sms = sm_count_of_current_device();
+  if (sms <= 0) return ADWIN_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (!status_init(flags, dev_status, s)) return ADWIN_ERR_CUDA;
+  if (launch_token_scores_bwd(logits, dtype, B, T, V, ld, tokens, window, rollout_len, lse, entropy, d_logprob,
+                              d_entropy, top_ids, d_top, K, flags, grad, grad_dtype, ld_grad, dev_status, sms,
+                              s) != cudaSuccess)
     return ADWIN_ERR_CUDA;
   return ADWIN_OK;
 }

@@ -107,6 +107,19 @@ cudaError_t launch_drift_curves(const float* entropy, const int32_t* rank,
                                 const int32_t* ks, int32_t K, int32_t* worst, double* survival,
                                 double* bf_mean, int32_t* n_active, cudaStream_t s);
 
+// Scores of given tokens (token_scores.cu).  entropy, lse, rest, d_*: may be null.
+cudaError_t launch_token_scores(const void* logits, int dtype, int64_t B, int64_t T, int64_t V, int64_t ld,
+                                const int32_t* tokens, const int32_t* window, const int32_t* rollout_len,
+                                int K, float* logprob, float* entropy, float* lse, int32_t* top_ids,
+                                float* top_logprobs, float* rest, int32_t* status, int sm_count,
+                                cudaStream_t s);
+cudaError_t launch_token_scores_bwd(const void* logits, int dtype, int64_t B, int64_t T, int64_t V, int64_t ld,
+                                    const int32_t* tokens, const int32_t* window, const int32_t* rollout_len,
+                                    const float* lse, const float* entropy, const float* d_logprob,
+                                    const float* d_entropy, const int32_t* top_ids, const float* d_top, int K,
+                                    int flags, void* grad, int grad_dtype, int64_t ld_grad, int32_t* status,
+                                    int sm_count, cudaStream_t s);
+
 // Fused LM-head form (lmhead.cu).
 size_t lmhead_workspace_bytes(int64_t B, int64_t T, int64_t V, int64_t ds, int64_t dt,
                               int64_t max_rows, bool want_grad);
