@@ -464,6 +464,44 @@ int adwin_token_logprobs_bwd(const void* logits, int dtype, int64_t B, int64_t T
                              const float* d_top, int32_t K, int flags, void* grad, int grad_dtype,
                              int64_t ld_grad, int32_t* dev_status, void* cuda_stream);
 
+/*
+ * Divergence of the student from a teacher known by its most likely alternatives alone, as a served
+ * teacher gives them (adwin_token_logprobs), with its gradient: one read of the student's logits.
+ * Every alternative is a category of its own, all other entries together are one more, the rest:
+ *   P_j = p_(id_j), P_r = the student's mass outside the list;   Q_j = exp(top_logprobs_j), Q_r likewise
+ *   D_c = log P_c - log Q_c
+ * For every processed row (t < E_b; with ADWIN_RANGE_FULL: t < R_b):
+ *   kl        = sum_c P_c D_c  (ADWIN_KL_REVERSE)   or   -sum_c Q_c D_c  (ADWIN_KL_FORWARD)
+ *   logratio  = D of the category of tokens[b,t]: the step-wise cost, an unbiased estimate of the
+ *               reverse divergence
+ *   gsq       = sum_k g_k^2
+ *   grad      = g for t < E_b:  g_k = grad_scale p_k (D_c(k) - kl)   (reverse),
+ *                               g_k = grad_scale (p_k - Q_c(k) p_k / P_c(k))   (forward)
+ * so kl, logratio, gsq go on to adwin_window_reduce and adwin_probe_align like those of
+ * adwin_opd_kl_fwd_bwd.  By the data-processing inequality kl is at most the divergence over the full vocabulary
+ * (Eq. 2), which it is with K = V and rest = -inf.  Rows that are not processed get 0.
+ *
+ * student_logits, tokens, window, rollout_len, grad_scale, grad_student, strides: as in
+ *                adwin_opd_kl_fwd_bwd, any alignment
+ * top_ids      : [B,T,K] int32, 1 <= K <= ADWIN_TOP_MAX; -1 stands for none.  Any other index outside
+ *                [0,V), and one that the row's list has already, is left out and raises
+ *                ADWIN_DEV_TOKEN_RANGE
+ * top_logprobs : [B,T,K] fp32, the teacher's log probabilities of these entries
+ * rest         : [B,T] fp32, the log of the teacher's mass outside the list, or NULL: what the list
+ *                leaves of 1, formed in 64 bits and at least 2^-24
+ * kl, logratio : [B,T] fp32, required.   gsq, lse: [B,T] fp32 or NULL
+ * flags        : ADWIN_ZERO_TAIL, ADWIN_RANGE_FULL, ADWIN_STATUS_INIT
+ * A row whose lse or kl is not finite raises ADWIN_DEV_NONFINITE (kl is +inf where one side has mass and
+ * the other none).  No workspace is needed.
+ */
+int adwin_opd_topk_kl_fwd_bwd(const void* student_logits, int dtype, int64_t B, int64_t T,
+                              int64_t V, int64_t ld, const int32_t* tokens, const int32_t* window,
+                              const int32_t* rollout_len, const int32_t* top_ids,
+                              const float* top_logprobs, const float* rest, int32_t K,
+                              float grad_scale, int kl_mode, int flags, void* grad_student,
+                              int grad_dtype, int64_t ld_grad, float* kl, float* logratio,
+                              float* gsq, float* lse, int32_t* dev_status, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,7 +33,8 @@ EXPORTS = ("adwin_version", "adwin_status_string", "adwin_workspace_bytes",
            "adwin_return_to_go", "adwin_opd_kl_fwd_bwd_weighted", "adwin_teacher_drift",
            "adwin_drift_curves", "adwin_lmhead_workspace_bytes", "adwin_opd_kl_lmhead_fwd_bwd",
            "adwin_diag_set_wait_limit_ns", "adwin_lmhead_align_workspace_bytes",
-           "adwin_lmhead_weight_align", "adwin_token_logprobs", "adwin_token_logprobs_bwd")
+           "adwin_lmhead_weight_align", "adwin_token_logprobs", "adwin_token_logprobs_bwd",
+           "adwin_opd_topk_kl_fwd_bwd")
 
 _lib = None
 
@@ -121,6 +122,10 @@ def lib():
         L.adwin_token_logprobs_bwd.argtypes = [vp, ctypes.c_int, i64, i64, i64, i64, vp, vp, vp, vp,
                                                vp, vp, vp, vp, vp, i32, ctypes.c_int, vp,
                                                ctypes.c_int, i64, vp, vp]
+        L.adwin_opd_topk_kl_fwd_bwd.restype = ctypes.c_int
+        L.adwin_opd_topk_kl_fwd_bwd.argtypes = [vp, ctypes.c_int, i64, i64, i64, i64, vp, vp, vp, vp,
+                                                vp, vp, i32, f32, ctypes.c_int, ctypes.c_int, vp,
+                                                ctypes.c_int, i64, vp, vp, vp, vp, vp, vp]
         L.adwin_diag_set_wait_limit_ns.restype = None
         L.adwin_diag_set_wait_limit_ns.argtypes = [ctypes.c_uint64]
         _lib = L
@@ -617,3 +622,44 @@ def adwin_token_logprobs_bwd(logits, tokens, lse, window=None, rollout_len=None,
         _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _ptr(top_ids), _ptr(d_top), K, int(flags),
         _ptr(grad), gdt, ld_grad, _ptr(dev_status), stream))
     return SimpleNamespace(grad=grad, dev_status=dev_status)
+
+
+def adwin_opd_topk_kl_fwd_bwd(student, tokens, top_ids, top_logprobs, window, rollout_len=None, *,
+                              rest=None, grad_scale=1.0, kl_mode=KL_REVERSE, flags=0, grad=None,
+                              grad_dtype=None, want_gsq=True, want_lse=False, dev_status=None):
+    """Windowed divergence from a teacher known by its alternatives, forward + backward (adwin.h).
+
+    student: [B,T,V] CUDA tensor (fp32 or bf16), last dim contiguous, rows at a uniform stride.
+    top_ids [B,T,K] int32, top_logprobs [B,T,K] fp32, rest [B,T] fp32 or None: what
+    ``adwin_token_logprobs`` returned for the teacher.  ``grad`` / ``grad_dtype`` and the returned
+    namespace (kl, logratio, gsq, lse_s, grad, dev_status) as in ``adwin_opd_kl_fwd_bwd``.
+    """
+    B, T, V, ld = _logit_rows(student)
+    dev = student.device
+    stream = _stream(dev)
+    _int32_arg("tokens", tokens, (B, T), dev)
+    _int32_arg("window", window, (B,), dev)
+    _int32_arg("rollout_len", rollout_len, (B,), dev)
+    K = top_ids.shape[-1]
+    if not 1 <= K <= TOP_MAX:
+        raise ValueError(f"between 1 and {TOP_MAX} alternatives")
+    _int32_arg("top_ids", top_ids, (B, T, K), dev)
+    _f32_arg("top_logprobs", top_logprobs, (B, T, K), dev)
+    _f32_arg("rest", rest, (B, T), dev)
+    if grad is None and grad_dtype is not None:
+        grad = torch.empty((B, T, V), dtype=grad_dtype, device=dev)
+    dt, gdt, ld_grad = _dtype_code(student.dtype), 0, 0
+    if grad is not None:
+        if tuple(grad.shape) != (B, T, V) or grad.device != dev:
+            raise ValueError("grad must have the logits' shape and device")
+        gdt, ld_grad = _dtype_code(grad.dtype), _logit_rows(grad)[3]
+    dev_status, flags = _own_status(dev_status, dev, B * T, flags)
+    s = _scalars(2 + (1 if want_gsq else 0) + (1 if want_lse else 0), B, T, dev)
+    o = SimpleNamespace(kl=s[0], logratio=s[1], gsq=s[2] if want_gsq else None,
+                        lse_s=s[-1] if want_lse else None, grad=grad, dev_status=dev_status)
+    _check(lib().adwin_opd_topk_kl_fwd_bwd(
+        _ptr(student), dt, B, T, V, ld, _ptr(tokens), _ptr(window), _ptr(rollout_len), _ptr(top_ids),
+        _ptr(top_logprobs), _ptr(rest), K, float(grad_scale), int(kl_mode), int(flags), _ptr(grad),
+        gdt, ld_grad, _ptr(o.kl), _ptr(o.logratio), _ptr(o.gsq), _ptr(o.lse_s), _ptr(dev_status),
+        stream))
+    return o

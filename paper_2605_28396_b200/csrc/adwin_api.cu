@@ -224,6 +224,42 @@ int adwin_token_logprobs_bwd(const void* logits, int dtype, int64_t B, int64_t T
   return ADWIN_OK;
 }
 
+int adwin_opd_topk_kl_fwd_bwd(const void* student_logits, int dtype, int64_t B, int64_t T,
+                              int64_t V, int64_t ld, const int32_t* tokens, const int32_t* window,
+                              const int32_t* rollout_len, const int32_t* top_ids,
+                              const float* top_logprobs, const float* rest, int32_t K,
+                              float grad_scale, int kl_mode, int flags, void* grad_student,
+                              int grad_dtype, int64_t ld_grad, float* kl, float* logratio,
+                              float* gsq, float* lse, int32_t* dev_status, void* cuda_stream) {
+  if (dtype != ADWIN_F32 && dtype != ADWIN_BF16) return ADWIN_ERR_DTYPE;
+  if (kl_mode != ADWIN_KL_REVERSE && kl_mode != ADWIN_KL_FORWARD) return ADWIN_ERR_DTYPE;
+  if (flags & ~(ADWIN_ZERO_TAIL | ADWIN_RANGE_FULL | ADWIN_STATUS_INIT)) return ADWIN_ERR_DTYPE;
+  if (grad_student && grad_dtype != ADWIN_F32 && grad_dtype != ADWIN_BF16) return ADWIN_ERR_DTYPE;
+  if (B < 0 || T < 0 || B > kMaxB || T > kMaxT || V < 1 || V > kMaxV || ld < V || K < 1 || K > ADWIN_TOP_MAX)
+    return ADWIN_ERR_SHAPE;
+  if (grad_student && ld_grad < V) return ADWIN_ERR_SHAPE;
+  if (!dev_status) return ADWIN_ERR_NULL;
+  if (B == 0 || T == 0) return ADWIN_OK;
+  if (!student_logits || !tokens || !window || !top_ids || !top_logprobs || !kl || !logratio)
+    return ADWIN_ERR_NULL;
+  if (!aligned(student_logits, elem_size(dtype)) || !aligned(tokens, 4) || !aligned(window, 4) ||
+      !aligned(rollout_len, 4) || !aligned(top_ids, 4) || !aligned(top_logprobs, 4) || !aligned(rest, 4) ||
+      !aligned(kl, 4) || !aligned(logratio, 4) || !aligned(gsq, 4) || !aligned(lse, 4) ||
+      !aligned(dev_status, 4) || (grad_student && !aligned(grad_student, elem_size(grad_dtype))))
+    return ADWIN_ERR_ALIGN;
+  // the rows to come are on their way while a row's gradient is written
+  if (grad_student == student_logits) return ADWIN_ERR_UNSUPPORTED;
+  const int sms = sm_count_of_current_device();
+  if (sms <= 0) return ADWIN_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (!status_init(flags, dev_status, s)) return ADWIN_ERR_CUDA;
+  if (launch_topk_kl(student_logits, dtype, B, T, V, ld, tokens, window, rollout_len, top_ids, top_logprobs,
+                     rest, K, grad_scale, kl_mode, flags, grad_student, grad_dtype, ld_grad, kl, logratio,
+                     gsq, lse, dev_status, sms, s) != cudaSuccess)
+    return ADWIN_ERR_CUDA;
+  return ADWIN_OK;
+}
+
 }  // extern "C"
 
 namespace adwin {

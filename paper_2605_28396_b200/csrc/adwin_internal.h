@@ -120,6 +120,14 @@ cudaError_t launch_token_scores_bwd(const void* logits, int dtype, int64_t B, in
                                     int flags, void* grad, int grad_dtype, int64_t ld_grad, int32_t* status,
                                     int sm_count, cudaStream_t s);
 
+// Divergence from a teacher known by its alternatives (topk_kl.cu).
+cudaError_t launch_topk_kl(const void* logits, int dtype, int64_t B, int64_t T, int64_t V, int64_t ld,
+                           const int32_t* tokens, const int32_t* window, const int32_t* rollout_len,
+                           const int32_t* top_ids, const float* top_logprobs, const float* rest, int K,
+                           float alpha, int kl_mode, int flags, void* grad, int grad_dtype, int64_t ld_grad,
+                           float* kl, float* logratio, float* gsq, float* lse, int32_t* status,
+                           int sm_count, cudaStream_t s);
+
 // Fused LM-head form (lmhead.cu).
 size_t lmhead_workspace_bytes(int64_t B, int64_t T, int64_t V, int64_t ds, int64_t dt,
                               int64_t max_rows, bool want_grad);

@@ -24,7 +24,7 @@
 // entries of the second kind are written again once the slice is done.
 #include "adwin_common.cuh"
 #include "adwin_internal.h"
-#include "kl_pairs.cuh"
+#include "exp_sums.cuh"
 #include "row_list.cuh"
 
 namespace adwin {
@@ -34,15 +34,6 @@ constexpr int kUnroll = 8;       // 16-byte loads in flight per thread
 constexpr int kSlots = 12;       // units of a thread, at most
 constexpr int kCand = 384;       // entries that can be ranked at once
 constexpr int kMaxClusterX = 8;
-constexpr float kLn2 = 0.69314718055994531f;
-constexpr float kLowest = -3.402823466e38f;
-constexpr float kNil = -150.f;   // 2^kNil is zero
-
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
 // Order of floats as order of whole numbers, and back.
 __device__ __forceinline__ int order_key(float z) {
   const int b = __float_as_int(z + 0.f);
@@ -85,27 +76,6 @@ struct Mass {
     }
   }
 };
-
-template <int U>
-__device__ __forceinline__ float group_max(const uint4 (&v)[U], __nv_bfloat16*) {
-  __nv_bfloat162 m = __float2bfloat162_rn(-INFINITY);
-#pragma unroll
-  for (int k = 0; k < U; ++k) {
-    const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m = __hmax2(m, reinterpret_cast<const __nv_bfloat162&>(w[j]));
-  }
-  return fmaxf(__low2float(m), __high2float(m));
-}
-template <int U>
-__device__ __forceinline__ float group_max(const uint4 (&v)[U], float*) {
-  float m = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < U; ++k)
-    m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(v[k].x)), fmaxf(__uint_as_float(v[k].y), __uint_as_float(v[k].z))),
-              __uint_as_float(v[k].w));
-  return m;
-}
 
 // 2^((z - m) log2 e) and its exponent of a pair.  The difference is formed first, so that an entry at
 // the reference has the exponent 0 whatever its size; masked entries (-inf, the lowest value) end
@@ -151,7 +121,7 @@ struct ScoreParams {
 };
 
 // What a CTA of a cluster hands to the first one.
-struct SliceResult {
+struct alignas(16) SliceResult {
   float m, s, a;
   Mass rest;
   int n;                 // entries of its list
@@ -449,6 +419,8 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
       p.top_logprobs[r * K + j] = 0.f;
     }
   });
+
+  if (C > 1) cluster_sync_all();   // every CTA is there before anything is written to one
 
   const int64_t rows = sh.list.count(p.range);
   for (int64_t n = blockIdx.x / C; n < rows; n += gridDim.x / C) {

@@ -108,9 +108,13 @@ def topk_kl(z, y, ids, lq, rest, forward, alpha=1.0):
         if forward:
             terms = -times(torch.exp(lQ), D)
             kl[i] = terms.sum()
-            g = times(p[i], 1.0 - torch.exp(-D[cat]))
+            # p_k / P_r, formed among the entries of the rest: their mass may be nothing to the whole
+            zo = torch.where(outside, z[i], -math.inf)
+            mo, so = log_parts(zo)
+            share = torch.exp(lr) * torch.exp((zo - mo) - so) if torch.isfinite(so) else torch.zeros_like(zo)
+            g = p[i] - share
             g[j] = P[:-1] - torch.exp(q)
-            size[i] = p[i] + times(p[i], torch.exp(-D[cat]))
+            size[i] = p[i] + share
             size[i][j] = P[:-1] + torch.exp(q)
         else:
             terms = times(P, D)
@@ -123,7 +127,7 @@ def topk_kl(z, y, ids, lq, rest, forward, alpha=1.0):
         gsq[i] = (grad[i] ** 2).sum()
         yi = int(y[i])
         c[i] = D[cat[yi]] if 0 <= yi < V else math.nan
-    return dict(kl=kl, logratio=c, gsq=gsq, lse=lse, grad=grad, size=size, size_kl=size_kl)
+    return dict(kl=kl, logratio=c, gsq=gsq, lse=lse, grad=grad, size=size, size_kl=size_kl, p=p)
 
 
 def quantize(x):
