@@ -502,6 +502,43 @@ int adwin_opd_topk_kl_fwd_bwd(const void* student_logits, int dtype, int64_t B, 
                               int grad_dtype, int64_t ld_grad, float* kl, float* logratio,
                               float* gsq, float* lse, int32_t* dev_status, void* cuda_stream);
 
+/*
+ * Rows to 8 bits with a step each: the activations of a product in 8-bit integers (a step per token), and,
+ * once, its weights (a step per output channel).
+ *   scale[i] = max_k |x[i,k]| / 127,   q[i,k] = x[i,k] / scale[i] rounded to the nearest whole number, ties
+ *   to even, both divisions correctly rounded in fp32;   q = 0 where scale is 0
+ * x            : [M,d], element type `dtype`, row stride ldx >= d elements, any alignment
+ * q            : [M,d] int8, row stride ldq >= d bytes (multiples of 16 for adwin_linear_i8); bytes
+ *                behind a row's d are left as they are
+ * scale        : [M] fp32
+ * flags        : ADWIN_STATUS_INIT
+ * A row with an infinity or a NaN gets q = 0, scale = NaN and raises ADWIN_DEV_NONFINITE.
+ * The paper has no counterpart: its teacher is frozen, and its output embedding the largest matrix
+ * that scoring a rollout reads.
+ */
+int adwin_quantize_rows_i8(const void* x, int dtype, int64_t M, int64_t d, int64_t ldx, int8_t* q,
+                           int64_t ldq, float* scale, int flags, int32_t* dev_status,
+                           void* cuda_stream);
+
+/*
+ * Product in 8-bit integers with a scale per token and per channel:
+ *   out[m,n] = (sum_k x[m,k] w[n,k]) * (x_scale[m] * w_scale[n])
+ * the sum exact in whole numbers, then rounded to fp32 and once more by the scales' product and
+ * the multiplication, at last to out_dtype: with w the frozen teacher's output embedding, the logits that
+ * adwin_token_logprobs reads.  There is no backward pass: nothing here is trained.
+ *
+ * x            : [M,d] int8, row stride ldx;  w : [N,d] int8, row stride ldw; both 16-byte aligned, strides
+ *                multiples of 16; bytes behind a row's d are not used
+ * x_scale [M], w_scale [N] fp32
+ * out          : [M,N] of out_dtype (ADWIN_F32 / ADWIN_BF16), row stride ldo >= N, any alignment
+ * d            : 1 <= d < 131072 (the sum stays below 2^31)
+ * flags        : ADWIN_STATUS_INIT
+ * It runs on the tensor cores; a wait that runs out raises ADWIN_DEV_TIMEOUT.
+ */
+int adwin_linear_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw,
+                    const float* w_scale, int64_t M, int64_t N, int64_t d, void* out, int out_dtype,
+                    int64_t ldo, int flags, int32_t* dev_status, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

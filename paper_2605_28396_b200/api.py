@@ -34,7 +34,7 @@ EXPORTS = ("adwin_version", "adwin_status_string", "adwin_workspace_bytes",
            "adwin_drift_curves", "adwin_lmhead_workspace_bytes", "adwin_opd_kl_lmhead_fwd_bwd",
            "adwin_diag_set_wait_limit_ns", "adwin_lmhead_align_workspace_bytes",
            "adwin_lmhead_weight_align", "adwin_token_logprobs", "adwin_token_logprobs_bwd",
-           "adwin_opd_topk_kl_fwd_bwd")
+           "adwin_opd_topk_kl_fwd_bwd", "adwin_quantize_rows_i8", "adwin_linear_i8")
 
 _lib = None
 
@@ -126,6 +126,12 @@ def lib():
         L.adwin_opd_topk_kl_fwd_bwd.argtypes = [vp, ctypes.c_int, i64, i64, i64, i64, vp, vp, vp, vp,
                                                 vp, vp, i32, f32, ctypes.c_int, ctypes.c_int, vp,
                                                 ctypes.c_int, i64, vp, vp, vp, vp, vp, vp]
+        L.adwin_quantize_rows_i8.restype = ctypes.c_int
+        L.adwin_quantize_rows_i8.argtypes = [vp, ctypes.c_int, i64, i64, i64, vp, i64, vp,
+                                             ctypes.c_int, vp, vp]
+        L.adwin_linear_i8.restype = ctypes.c_int
+        L.adwin_linear_i8.argtypes = [vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, ctypes.c_int, i64,
+                                      ctypes.c_int, vp, vp]
         L.adwin_diag_set_wait_limit_ns.restype = None
         L.adwin_diag_set_wait_limit_ns.argtypes = [ctypes.c_uint64]
         _lib = L
@@ -663,3 +669,66 @@ def adwin_opd_topk_kl_fwd_bwd(student, tokens, top_ids, top_logprobs, window, ro
         gdt, ld_grad, _ptr(o.kl), _ptr(o.logratio), _ptr(o.gsq), _ptr(o.lse_s), _ptr(dev_status),
         stream))
     return o
+
+
+def _matrix(name, t):
+    """Rows, columns and row stride of a [...,d] tensor whose rows lie at one uniform stride."""
+    if t.dim() < 2:
+        raise ValueError(f"{name}: at least two dimensions")
+    d, M, ld, first = t.shape[-1], 1, t.shape[-1], True
+    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n != 1:
+            if first:
+                ld, first = st, False
+            elif st != M * ld:
+                raise ValueError(f"{name}: rows must lie at one uniform stride")
+        M *= n
+    if (d > 1 and t.stride(-1) != 1) or ld < d:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return M, d, ld
+
+
+def adwin_quantize_rows_i8(x, *, flags=0, dev_status=None):
+    """Rows of x ([...,d], fp32 or bf16) in 8 bits with a step each (see include/adwin.h): returns
+    (q, scale), q [...,d] int8 with its rows padded to 16 bytes, scale [...] fp32."""
+    M, d, ld = _matrix("x", x)
+    dev = x.device
+    stream = _stream(dev)
+    if d < 1:
+        raise ValueError("x: empty rows")
+    dt = _dtype_code(x.dtype)
+    dev_status, flags = _own_status(dev_status, dev, M, flags)
+    ldq = -(-d // 16) * 16
+    q = torch.empty((*x.shape[:-1], ldq), dtype=torch.int8, device=dev)
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
+    _check(lib().adwin_quantize_rows_i8(_ptr(x), dt, M, d, ld, _ptr(q), ldq, _ptr(scale), int(flags),
+                                        _ptr(dev_status), stream))
+    return (q if ldq == d else q[..., :d]), scale
+
+
+def adwin_linear_i8(x, x_scale, w, w_scale, *, out=None, out_dtype=torch.bfloat16, flags=0,
+                    dev_status=None):
+    """Product of 8-bit rows with their scales (see include/adwin.h): x [...,d], w [V,d] int8 as
+    ``adwin_quantize_rows_i8`` returns them, x_scale [...], w_scale [V] fp32.  Returns out [...,V]
+    (``out``, or a new tensor of ``out_dtype``)."""
+    M, d, ldx = _matrix("x", x)
+    N, dw, ldw = _matrix("w", w)
+    dev = x.device
+    stream = _stream(dev)
+    if w.dim() != 2 or dw != d or x.dtype != torch.int8 or w.dtype != torch.int8 or w.device != dev:
+        raise ValueError("x and w must be int8 tensors of one row length on one device")
+    _f32_arg("x_scale", x_scale, tuple(x.shape[:-1]), dev)
+    _f32_arg("w_scale", w_scale, (N,), dev)
+    shape = (*x.shape[:-1], N)
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=dev)
+    if tuple(out.shape) != shape or out.device != dev:
+        raise ValueError("out: wrong shape or device")
+    ldo = _matrix("out", out)[2]
+    # a single row's stride is never used: any multiple of 16 will do
+    ldx, ldw = (-(-d // 16) * 16 if n <= 1 else ld for n, ld in ((M, ldx), (N, ldw)))
+    odt = _dtype_code(out.dtype)
+    dev_status, flags = _own_status(dev_status, dev, M, flags)
+    _check(lib().adwin_linear_i8(_ptr(x), ldx, _ptr(x_scale), _ptr(w), ldw, _ptr(w_scale), M, N, d,
+                                 _ptr(out), odt, ldo, int(flags), _ptr(dev_status), stream))
+    return out

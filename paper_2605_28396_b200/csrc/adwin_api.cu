@@ -18,6 +18,7 @@ constexpr int kKnownFlags =
 constexpr int64_t kMaxB = int64_t(1) << 24;
 constexpr int64_t kMaxT = int64_t(1) << 24;
 constexpr int64_t kMaxV = int64_t(1) << 28;
+constexpr int64_t kMaxRows = int64_t(1) << 30;
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t elem_size(int dtype) { return dtype == ADWIN_F32 ? 4 : 2; }
@@ -256,6 +257,48 @@ int adwin_opd_topk_kl_fwd_bwd(const void* student_logits, int dtype, int64_t B, 
   if (launch_topk_kl(student_logits, dtype, B, T, V, ld, tokens, window, rollout_len, top_ids, top_logprobs,
                      rest, K, grad_scale, kl_mode, flags, grad_student, grad_dtype, ld_grad, kl, logratio,
                      gsq, lse, dev_status, sms, s) != cudaSuccess)
+    return ADWIN_ERR_CUDA;
+  return ADWIN_OK;
+}
+
+int adwin_quantize_rows_i8(const void* x, int dtype, int64_t M, int64_t d, int64_t ldx, int8_t* q,
+                           int64_t ldq, float* scale, int flags, int32_t* dev_status,
+                           void* cuda_stream) {
+  if (dtype != ADWIN_F32 && dtype != ADWIN_BF16) return ADWIN_ERR_DTYPE;
+  if (flags & ~ADWIN_STATUS_INIT) return ADWIN_ERR_DTYPE;
+  if (M < 0 || M > kMaxRows || d < 1 || d > kMaxV || ldx < d || ldq < d) return ADWIN_ERR_SHAPE;
+  if (!dev_status) return ADWIN_ERR_NULL;
+  if (M == 0) return ADWIN_OK;
+  if (!x || !q || !scale) return ADWIN_ERR_NULL;
+  if (!aligned(x, elem_size(dtype)) || !aligned(scale, 4) || !aligned(dev_status, 4)) return ADWIN_ERR_ALIGN;
+  const int sms = sm_count_of_current_device();
+  if (sms <= 0) return ADWIN_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (!status_init(flags, dev_status, s)) return ADWIN_ERR_CUDA;
+  if (launch_quantize_rows(x, dtype, M, d, ldx, q, ldq, scale, dev_status, sms, s) != cudaSuccess)
+    return ADWIN_ERR_CUDA;
+  return ADWIN_OK;
+}
+
+int adwin_linear_i8(const int8_t* x, int64_t ldx, const float* x_scale, const int8_t* w, int64_t ldw,
+                    const float* w_scale, int64_t M, int64_t N, int64_t d, void* out, int out_dtype,
+                    int64_t ldo, int flags, int32_t* dev_status, void* cuda_stream) {
+  if (out_dtype != ADWIN_F32 && out_dtype != ADWIN_BF16) return ADWIN_ERR_DTYPE;
+  if (flags & ~ADWIN_STATUS_INIT) return ADWIN_ERR_DTYPE;
+  if (M < 0 || M > kMaxRows || N < 1 || N > kMaxV || d < 1 || d >= 131072 || ldx < d || ldw < d || ldo < N)
+    return ADWIN_ERR_SHAPE;
+  if (!dev_status) return ADWIN_ERR_NULL;
+  if (M == 0) return ADWIN_OK;
+  if (!x || !x_scale || !w || !w_scale || !out) return ADWIN_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(w, 16) || ldx % 16 || ldw % 16 || !aligned(x_scale, 4) ||
+      !aligned(w_scale, 4) || !aligned(out, elem_size(out_dtype)) || !aligned(dev_status, 4))
+    return ADWIN_ERR_ALIGN;
+  const int sms = sm_count_of_current_device();
+  if (sms <= 0) return ADWIN_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  if (!status_init(flags, dev_status, s)) return ADWIN_ERR_CUDA;
+  if (launch_linear_i8(x, ldx, x_scale, w, ldw, w_scale, M, N, d, out, out_dtype, ldo, dev_status, sms, s) !=
+      cudaSuccess)
     return ADWIN_ERR_CUDA;
   return ADWIN_OK;
 }

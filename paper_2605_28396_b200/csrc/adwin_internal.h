@@ -128,6 +128,13 @@ cudaError_t launch_topk_kl(const void* logits, int dtype, int64_t B, int64_t T, 
                            float* kl, float* logratio, float* gsq, float* lse, int32_t* status,
                            int sm_count, cudaStream_t s);
 
+// Products in 8-bit integers (int8_linear.cu).
+cudaError_t launch_quantize_rows(const void* x, int dtype, int64_t M, int64_t d, int64_t ldx, int8_t* q,
+                                 int64_t ldq, float* step, int32_t* status, int sm_count, cudaStream_t s);
+cudaError_t launch_linear_i8(const int8_t* x, int64_t ldx, const float* step_x, const int8_t* w, int64_t ldw,
+                             const float* step_w, int64_t M, int64_t N, int64_t d, void* out, int out_dtype,
+                             int64_t ldo, int32_t* status, int sm_count, cudaStream_t s);
+
 // Fused LM-head form (lmhead.cu).
 size_t lmhead_workspace_bytes(int64_t B, int64_t T, int64_t V, int64_t ds, int64_t dt,
                               int64_t max_rows, bool want_grad);

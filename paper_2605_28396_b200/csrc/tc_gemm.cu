@@ -48,17 +48,25 @@ EncodeTiledFn encode_tiled() {
 
 }  // namespace
 
-bool make_map(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t pitch,
-              int box_rows) {
+static bool make_map_of(CUtensorMapDataType type, int entry_bytes, CUtensorMap* m, const void* base,
+                        int64_t cols, int64_t rows, int64_t pitch, int box_rows) {
   EncodeTiledFn fn = encode_tiled();
   if (!fn || rows < 1 || cols < 1) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)pitch * 2};
-  const cuuint32_t box[2] = {(cuuint32_t)kBK, (cuuint32_t)box_rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)pitch * entry_bytes};
+  const cuuint32_t box[2] = {(cuuint32_t)(kBK * 2 / entry_bytes), (cuuint32_t)box_rows};
   const cuuint32_t estr[2] = {1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box,
+  return fn(m, type, 2, const_cast<void*>(base), dims, strides, box,
             estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool make_map(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t pitch,
+              int box_rows) {
+  return make_map_of(CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m, base, cols, rows, pitch, box_rows);
+}
+bool make_map_i8(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t pitch,
+                 int box_rows) {
+  return make_map_of(CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, m, base, cols, rows, pitch, box_rows);
 }
 
 namespace {

@@ -349,6 +349,9 @@ __device__ __forceinline__ void pair_drain_loads(Ctrl* ctrl, uint32_t it) {
 // 128-byte swizzle; out-of-range elements read as zero.
 bool make_map(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t pitch,
               int box_rows);
+// The same for 8-bit entries, boxes of 128 columns.
+bool make_map_i8(CUtensorMap* m, const void* base, int64_t cols, int64_t rows, int64_t pitch,
+                 int box_rows);
 
 // Launches a pair kernel: clusters of two CTAs on all SMs.
 template <typename K, typename... Args>
