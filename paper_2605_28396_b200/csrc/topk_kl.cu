@@ -7,17 +7,18 @@
 //   forward  KL = sum_c Q_c (log Q_c - log P_c),    g_k = alpha (p_k - Q_c(k) p_k / P_c(k)).
 // So every entry of the rest gets p_k times one coefficient of the row.  P_r is summed over the entries
 // of the rest alone (1 - sum_j P_j would have no correct digit where the list holds nearly everything):
-// a thread masks the listed entries out of the pieces they lie in, of which it has a list in shared
+// a thread masks the listed entries out of the pieces they lie in, which it finds in a chain in shared
 // memory, empty for most threads.  |g|^2 needs sum p_k^2 over the rest beside it.
 //
-// A row is read once: a thread fetches 16-byte pieces with cp.async into slots of its own in shared
-// memory and takes them from there in both sweeps, so the copies need no barrier.  A slot that
-// the second sweep has read is refilled at once with a piece of a row to come; what a CTA (or a cluster of
-// them, a slice of the row each) has in flight is the ring's room beyond one row.  Between the sweeps
-// the warps meet once, at the cluster's barrier, and each derives the row's scalars for itself.  One
-// more warp looks the rows up, prepares the lists of the row after next, sums the few entries beside
-// the 16-byte pieces and writes the row's outputs.
-// Rows that no ring holds (kStream) are read twice.
+// A row is read from memory once: its second read comes while it is still in L2 (the first asks for it to be
+// kept, the second and the gradient's stores to go first; a CTA, or a cluster with a slice of the
+// row each, has one row at a time).  Several CTAs per SM fill one another's gaps between the sweeps.  The warps meet
+// twice a row: when its sums are complete (a cluster's CTAs too), and when one more warp has made the row's
+// scalars of them.  That warp also looks the rows up, sums the few entries beside the 16-byte
+// pieces and writes the outputs; another prepares the lists, in three steps a row apart (index,
+// logit, chains and sums), so that it never waits for its loads.
+#include <atomic>
+
 #include "adwin_common.cuh"
 #include "adwin_internal.h"
 #include "exp_sums.cuh"
@@ -28,6 +29,9 @@ namespace {
 
 constexpr int kGroup = 4;        // pieces a thread takes at a time
 constexpr int kMaxCtas = 8;      // of a cluster
+constexpr int kInfos = 8;        // rows that are known at a time
+constexpr int kPerLane = ADWIN_TOP_MAX / 32;
+constexpr int kChains = 128;
 
 struct TopkParams {
   const void* logits;
@@ -45,7 +49,6 @@ struct TopkParams {
   int64_t ld_grad;
   float *kl, *logratio, *gsq, *lse;   // gsq, lse: may be null
   int32_t* status;
-  int n, ring;               // slots of a row, slots of the ring
 };
 
 // What the threads have to know of a row.
@@ -53,23 +56,26 @@ struct RowInfo {
   const char* row;       // its logits, or null: no more rows
   char* out;             // its gradient, or null
   int64_t r;
-  int64_t entry0;        // vocabulary index of the slice's first piece
-  int head, tail;
+  int entry0;            // vocabulary index of the slice's first piece
   int np;                // pieces of the slice
+  int head, tail;        // entries beside the row's pieces that belong to this CTA
   int y;
 };
 
-// The listed entries of a row.  Every entry is in the chain of one thread, that whose pieces hold it
-// where there is one; an index that comes twice is found in its chain.
-template <int TH>
+// The listed entries of a row, in chains by the thread whose pieces hold them; an index that comes
+// twice is found in its chain.
 struct TopList {
   int32_t id[ADWIN_TOP_MAX];      // -1: none
   float z[ADWIN_TOP_MAX], lq[ADWIN_TOP_MAX];
   int32_t slot[ADWIN_TOP_MAX];    // where it lies among its thread's pieces, or -1: not in this CTA's
-  int16_t owner[ADWIN_TOP_MAX];   // the chain it is in, or -1
+  int16_t owner[ADWIN_TOP_MAX];   // its thread
   int16_t next[ADWIN_TOP_MAX];
-  int32_t first[TH];              // -1: an empty chain
+  int32_t counts[ADWIN_TOP_MAX];  // 0: none, or an index that the list has already
+  int32_t first[kChains];         // -1: an empty chain
   float lq_rest;
+  // Sums over the list, e_j = exp(z_j - zmax):  s = sum e_j;  and with x_j = (z_j - zmax) - lq_j
+  // a = sum e_j x_j (reverse) or sum Q_j x_j (forward), q = sum Q_j
+  float zmax, s, a, q;
 };
 
 struct alignas(16) SumRecord {   // (written to a cluster's other CTAs in one piece)
@@ -77,39 +83,53 @@ struct alignas(16) SumRecord {   // (written to a cluster's other CTAs in one pi
   float pad;
 };
 
+// Scalars of a row.
+struct TopScalars {
+  float M, ln_s, inv_s;   // reference, log and inverse of the whole sum against it
+  float kl, d_rest;
+  // g_k = alpha c_rest exp(z_k - m_rest) for entries of the rest: against their own largest, for
+  // the forward divergence divides by their mass, however far that is below the listed entries'
+  float m_rest, c_rest;
+  float gsq_rest;         // sum (g_k / alpha)^2 over them
+};
+
 template <int TH>
 struct TopkShared {
   static constexpr int kWarps = TH / 32 + 1;
   RowList list;
-  RowInfo info[4];
-  TopList<TH> lists[3];
+  RowInfo info[kInfos];
+  TopList lists[3];
+  TopScalars scalars;
   SumRecord rec[2][kMaxCtas * kWarps];
 };
 static_assert(alignof(TopkShared<128>) == 16 && sizeof(SumRecord) == 16, "records are stored 16 bytes at a time");
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// A row's first read and its second.
+__device__ __forceinline__ uint64_t keep_policy() {
+  uint64_t p;
+  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  return p;
 }
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// Waits until at most `pending` groups of this thread's copies are in flight (the instruction
-// takes a constant).
-__device__ __forceinline__ void copies_wait(int pending) {
-#define ADWIN_WAIT(n) case n: asm volatile("cp.async.wait_group " #n ";" ::: "memory"); break;
-  switch (pending) {
-    ADWIN_WAIT(1) ADWIN_WAIT(2) ADWIN_WAIT(3) ADWIN_WAIT(4) ADWIN_WAIT(5) ADWIN_WAIT(6) ADWIN_WAIT(7)
-    ADWIN_WAIT(8) ADWIN_WAIT(9) ADWIN_WAIT(10) ADWIN_WAIT(11) ADWIN_WAIT(12) ADWIN_WAIT(13)
-    ADWIN_WAIT(14) ADWIN_WAIT(15) ADWIN_WAIT(16) ADWIN_WAIT(17) ADWIN_WAIT(18) ADWIN_WAIT(19)
-    ADWIN_WAIT(20) ADWIN_WAIT(21) ADWIN_WAIT(22) ADWIN_WAIT(23) ADWIN_WAIT(24) ADWIN_WAIT(25)
-    default: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
-  }
-#undef ADWIN_WAIT
+__device__ __forceinline__ uint64_t drop_policy() {
+  uint64_t p;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
 }
-__device__ __forceinline__ uint4 read16(uint32_t addr) {
+__device__ __forceinline__ uint4 read16(const uint4* src, uint64_t policy) {
   uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr)
-               : "memory");
+  asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(src), "l"(policy));
   return v;
 }
+// A logit as it lies in memory, so that a register can wait for it.
+__device__ __forceinline__ uint32_t raw_logit(const void* row, int i, float*) {
+  return __ldg(static_cast<const uint32_t*>(row) + i);
+}
+__device__ __forceinline__ uint32_t raw_logit(const void* row, int i, __nv_bfloat16*) {
+  return __ldg(static_cast<const uint16_t*>(row) + i);
+}
+__device__ __forceinline__ float logit_of(uint32_t raw, float*) { return __uint_as_float(raw); }
+__device__ __forceinline__ float logit_of(uint32_t raw, __nv_bfloat16*) { return bf16lo(raw); }
 
 template <typename TIn>
 __device__ __forceinline__ uint4 masked_piece() {
@@ -147,22 +167,13 @@ struct RestSum {
       m = x;
     }
   }
-  __device__ __forceinline__ void add(f2_t z) {
-    const f2_t e = ex2_2(mul2(add2(z, splat2(-m)), splat2(kLog2e)));
+  __device__ __forceinline__ void add(f2_t z, f2_t neg_m) {
+    const f2_t e = ex2_2(mul2(add2(z, neg_m), splat2(kLog2e)));
     S = add2(S, e);
     Q = fma2(e, e, Q);
   }
 };
 
-// Scalars of a row, the same in every warp.
-struct TopScalars {
-  float M, ln_s, inv_s;   // reference, log and inverse of the whole sum against it
-  float kl, d_rest;
-  // g_k = alpha c_rest exp(z_k - m_rest) for entries of the rest: against their own largest, for
-  // the forward divergence divides by their mass, however far that is below the listed entries'
-  float m_rest, c_rest;
-  float gsq_rest;         // sum (g_k / alpha)^2 over them
-};
 // Gradient at a listed entry, before alpha.
 __device__ __forceinline__ float listed_grad(const TopScalars& t, float z, float lq, bool forward) {
   const float p = exp_below(z, t.M) * t.inv_s;
@@ -170,120 +181,16 @@ __device__ __forceinline__ float listed_grad(const TopScalars& t, float z, float
   return p == 0.f ? 0.f : p * ((((z - t.M) - t.ln_s) - lq) - t.kl);
 }
 
-template <typename TIn, typename TOut, int TH, bool STREAM>
+template <typename TIn, typename TOut, int TH>
 struct TopkCta {
   static constexpr int N = Elem<TIn>::N, NP = Pairs<TIn>::NP;
-  static constexpr int kWarps = TH / 32 + 1;
+  static constexpr int kWarps = TH / 32 + 1;   // those that sum
   const TopkParams& p;
   TopkShared<TH>& sh;
-  const uint32_t ring;         // shared address of the slots
   const int C, me, tid, lane, warp;
-  int64_t rows, cursor, step;
-
-  // Next row of this cluster becomes info[o % 4]; one warp.
-  __device__ __forceinline__ void look_up(int o) {
-    int64_t r = -1;
-    while (cursor < rows) {
-      r = sh.list.row(p.range, cursor);
-      cursor += step;
-      if (r >= 0) break;
-    }
-    RowInfo i = {};
-    i.r = r;
-    if (r >= 0) {
-      i.row = static_cast<const char*>(p.logits) + (size_t)r * p.ld * sizeof(TIn);
-      const RowPieces rp = RowPieces::of<TIn>(i.row, p.V);
-      const int64_t per = (rp.pieces + C - 1) / C, first = per * me < rp.pieces ? per * me : rp.pieces;
-      i.np = (int)(first + per < rp.pieces ? per : rp.pieces - first);
-      i.entry0 = rp.head + first * N;
-      i.head = me == 0 ? rp.head : 0;
-      i.tail = me == C - 1 ? rp.tail : 0;
-      i.y = p.tokens[r];
-      if (p.grad) {
-        const int64_t b = r / p.range.T;
-        const RowRange w = {p.window, p.rollout, p.range.B, p.range.T};
-        if (r - b * p.range.T < w.end(b)) i.out = static_cast<char*>(p.grad) + (size_t)r * p.ld_grad * sizeof(TOut);
-      }
-    }
-    if (lane == 0) sh.info[o & 3] = i;
-    __syncwarp();
-  }
-
-  // The list of the row of info[o % 4] into lists[o % 3]; one warp.
-  __device__ __forceinline__ void prepare(int o) {
-    TopList<TH>& l = sh.lists[o % 3];
-    const RowInfo& i = sh.info[o & 3];
-    const int K = p.K;
-    for (int j = lane; j < K; j += 32)      // (the list that was here)
-      if (l.owner[j] >= 0) l.first[l.owner[j]] = -1;
-    __syncwarp();
-    double left = 0.0;
-    for (int j = lane; j < K; j += 32) {
-      int32_t id = i.row ? p.top_ids[i.r * K + j] : -1;
-      if (id < -1 || (int64_t)id >= p.V) {
-        if (me == 0) atomicOr(p.status, (int32_t)ADWIN_DEV_TOKEN_RANGE);
-        id = -1;
-      }
-      int owner = -1, slot = -1;
-      if (id >= 0) {
-        const int64_t e = (int64_t)id - i.entry0;
-        if (e >= 0 && e < (int64_t)i.np * N) {
-          owner = (int)(e / N % TH);
-          slot = (int)(e / N / TH);
-        } else {
-          owner = id % TH;   // (any thread)
-        }
-      }
-      l.id[j] = id;
-      l.lq[j] = id >= 0 ? p.top_logprobs[i.r * K + j] : 0.f;
-      l.z[j] = id >= 0 ? Elem<TIn>::load1(i.row, id) : 0.f;
-      l.slot[j] = slot;
-      l.owner[j] = (int16_t)owner;
-      if (owner >= 0) l.next[j] = (int16_t)atomicExch(&l.first[owner], j);   // (the order of a chain does not matter)
-    }
-    __syncwarp();
-    uint32_t again = 0;
-    for (int j = lane, bit = 0; j < K; j += 32, ++bit) {
-      if (l.owner[j] < 0) continue;
-      for (int k = l.first[l.owner[j]]; k >= 0; k = l.next[k])
-        if (k < j && l.id[k] == l.id[j]) again |= 1u << bit;
-    }
-    __syncwarp();
-    for (int j = lane, bit = 0; j < K; j += 32, ++bit) {
-      if (again >> bit & 1) {
-        l.id[j] = -1;
-        l.slot[j] = -1;
-        if (me == 0) atomicOr(p.status, (int32_t)ADWIN_DEV_TOKEN_RANGE);
-      }
-      if (l.id[j] >= 0 && !p.rest) left += exp((double)l.lq[j]);
-    }
-    float lqr = 0.f;
-    if (p.rest) {
-      lqr = i.row ? p.rest[i.r] : 0.f;
-    } else {
-#pragma unroll
-      for (int s = 16; s > 0; s >>= 1) left += __shfl_xor_sync(0xffffffffu, left, s);
-      lqr = (float)log(fmax(1.0 - left, 5.9604644775390625e-8));   // 2^-24
-    }
-    if (lane == 0) l.lq_rest = lqr;
-    __syncwarp();
-  }
-
-  // An entry beside the slice's pieces that this lane of the extra warp holds, or -1.
-  __device__ __forceinline__ int64_t edge_of(const RowInfo& i) const {
-    if (lane < i.head) return lane;
-    if (lane >= 16 && lane - 16 < i.tail) return p.V - i.tail + (lane - 16);
-    return -1;
-  }
-  __device__ __forceinline__ int listed(const TopList<TH>& l, int64_t id) const {
-    int found = -1;
-    for (int j = 0; j < p.K; ++j)
-      if (l.id[j] == (int32_t)id) found = j;
-    return found;
-  }
 
   // Hands a warp's sum to every CTA of the cluster.
-  __device__ __forceinline__ void publish(int par, float m, float s, float q) {
+  __device__ __forceinline__ void publish(int par, float m, float s, float q) const {
     SumRecord* mine = &sh.rec[par][me * kWarps + warp];
     if (C == 1) {
       if (lane == 0) *mine = SumRecord{m, s, q, 0.f};
@@ -294,9 +201,74 @@ struct TopkCta {
   __device__ __forceinline__ void meet() const {
     if (C == 1) __syncthreads(); else cluster_sync_all();
   }
+  __device__ __forceinline__ const RowInfo& info_of(int o) const { return sh.info[o % kInfos]; }
 
-  // Every warp for itself, the same arithmetic in the same order.
-  __device__ __forceinline__ TopScalars scalars(int par, const TopList<TH>& l, float& gsq_listed) const {
+  // ------------------------------------------------------------------ the row's warp
+  struct Cursor {
+    int64_t n, rows, step;
+    int b;                     // sequence of the list that holds row n, or one before it
+  };
+  __device__ __forceinline__ void look_up(int o, Cursor& c) const {
+    int64_t r = -1;
+    if (p.range.listed()) {
+      if (c.n < c.rows) {
+        while (sh.list.off[c.b + 1] <= (int)c.n) ++c.b;
+        r = (int64_t)c.b * p.range.T + ((int)c.n - sh.list.off[c.b]);
+        c.n += c.step;
+      }
+    } else {
+      while (c.n < c.rows && r < 0) {
+        r = sh.list.row(p.range, c.n);
+        c.n += c.step;
+      }
+    }
+    RowInfo i = {};
+    i.r = r;
+    if (r >= 0) {
+      i.row = static_cast<const char*>(p.logits) + (size_t)r * p.ld * sizeof(TIn);
+      const RowPieces rp = RowPieces::of<TIn>(i.row, p.V);
+      const int pieces = (int)rp.pieces, per = (int)((uint32_t)(pieces + C - 1) / (uint32_t)C);
+      const int first = per * me < pieces ? per * me : pieces;
+      i.np = first + per < pieces ? per : pieces - first;
+      i.entry0 = rp.head + first * N;
+      i.head = me == 0 ? rp.head : 0;
+      i.tail = me == C - 1 ? rp.tail : 0;
+      i.y = __ldg(p.tokens + r);
+      if (p.grad) {
+        bool inside = true;
+        if (!p.range.window && p.window) {   // (otherwise every processed row has a gradient)
+          const int64_t b = r / p.range.T;
+          const RowRange w = {p.window, p.rollout, p.range.B, p.range.T};
+          inside = r - b * p.range.T < w.end(b);
+        }
+        if (inside) i.out = static_cast<char*>(p.grad) + (size_t)r * p.ld_grad * sizeof(TOut);
+      }
+    }
+    if (lane == 0) sh.info[o % kInfos] = i;
+    __syncwarp();
+  }
+
+  // An entry beside the slice's pieces that this lane holds, or -1, and its logit.
+  __device__ __forceinline__ int edge_of(const RowInfo& i) const {
+    if (lane < i.head) return lane;
+    if (lane >= 16 && lane - 16 < i.tail) return (int)p.V - i.tail + (lane - 16);
+    return -1;
+  }
+  __device__ __forceinline__ uint32_t edge_logit(int o) const {
+    const RowInfo& i = info_of(o);
+    const int e = i.row ? edge_of(i) : -1;
+    return e >= 0 ? raw_logit(i.row, e, static_cast<TIn*>(nullptr)) : 0u;
+  }
+  __device__ __forceinline__ int listed(const TopList& l, int e) const {
+    int found = -1;
+    if (__any_sync(0xffffffffu, e >= 0)) {
+      for (int j = p.K - 1; j >= 0; --j)
+        if (l.id[j] == e) found = j;          // (the first one counts)
+    }
+    return e >= 0 ? found : -1;
+  }
+
+  __device__ __forceinline__ TopScalars make_scalars(int par, const TopList& l) const {
     float m = kLowest;
     const int n = C * kWarps;
     for (int i = lane; i < n; i += 32) m = fmaxf(m, sh.rec[par][i].m);
@@ -308,238 +280,365 @@ struct TopkCta {
       s = fmaf(w, r.s, s);
       q = fmaf(w * w, r.q, q);
     }
-    s = lane_sum(s);
-    q = lane_sum(q);
-    float z[ADWIN_TOP_MAX / 32], lq[ADWIN_TOP_MAX / 32];
-    float M = m;
 #pragma unroll
-    for (int k = 0; k < ADWIN_TOP_MAX / 32; ++k) {
-      const int j = lane + 32 * k;
-      const bool there = j < p.K && l.id[j] >= 0;
-      z[k] = there ? l.z[j] : -INFINITY;
-      lq[k] = there ? l.lq[j] : -INFINITY;
-      M = fmaxf(M, z[k]);
+    for (int o = 16; o > 0; o >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, o);
+      q += __shfl_xor_sync(0xffffffffu, q, o);
     }
-    M = warp_max(M);
-    float st = 0.f;
-#pragma unroll
-    for (int k = 0; k < ADWIN_TOP_MAX / 32; ++k) st += exp_below(z[k], M);   // (-inf: 0, NaN stays)
-    st = lane_sum(st);
+    const float zmax = l.zmax, le = l.s, la = l.a, lqs = l.q, lqr = l.lq_rest;
     TopScalars t;
+    const float M = fmaxf(m, zmax), wr = exp_below(m, M), wt = exp_below(zmax, M);
+    const float sum = fmaf(wr, s, wt * le);
     t.M = M;
-    const float wr = exp_below(m, M), sum = fmaf(wr, s, st);
     t.ln_s = logf(sum);
     t.inv_s = 1.f / sum;
-    const float pr = wr * s * t.inv_s, lqr = l.lq_rest;
-    const float lpr = s > 0.f ? (m - M) + (logf(s) - t.ln_s) : -INFINITY;
-    t.d_rest = lpr - lqr;
     t.m_rest = m;
-    float kl = 0.f;
-#pragma unroll
-    for (int k = 0; k < ADWIN_TOP_MAX / 32; ++k) {
-      const int j = lane + 32 * k;
-      if (j >= p.K || l.id[j] < 0) continue;
-      const float lp = (z[k] - M) - t.ln_s, pj = exp_below(z[k], M) * t.inv_s, qj = expf(lq[k]);
-      if (p.forward) kl += qj == 0.f ? 0.f : qj * (lq[k] - lp);
-      else kl += pj == 0.f ? 0.f : pj * (lp - lq[k]);
-    }
-    kl = lane_sum(kl);
+    const float lpr = s > 0.f ? (m - M) + (logf(s) - t.ln_s) : -INFINITY, pr = wr * s * t.inv_s;
+    t.d_rest = lpr - lqr;
+    const float shift = (zmax - M) - t.ln_s;   // log P_j - lq_j = x_j + shift
+    float kl;
     t.c_rest = 0.f;   // (no entry is left, or none with any mass)
     if (p.forward) {
       const float qr = expf(lqr);
+      kl = -(lqs == 0.f ? la : fmaf(lqs, shift, la));
       kl += qr == 0.f ? 0.f : qr * -t.d_rest;
       if (s != 0.f) t.c_rest = wr * t.inv_s - qr / s;
-    } else if (s != 0.f) {
-      kl += pr == 0.f ? 0.f : pr * t.d_rest;
-      t.c_rest = wr == 0.f ? 0.f : (t.d_rest - kl) * (wr * t.inv_s);
+    } else {
+      const float pt = wt * t.inv_s;
+      kl = pt == 0.f || le == 0.f ? 0.f : pt * fmaf(le, shift, la);
+      if (s != 0.f) {
+        kl += pr == 0.f ? 0.f : pr * t.d_rest;
+        t.c_rest = wr == 0.f ? 0.f : (t.d_rest - kl) * (wr * t.inv_s);
+      }
     }
+    if (!(sum > 0.f)) kl = t.c_rest = __int_as_float(0x7fc00000);   // nothing is left, or NaN
     t.gsq_rest = t.c_rest * t.c_rest * q;
     t.kl = kl;
-    gsq_listed = 0.f;
-    if (warp == kWarps - 1) {
-#pragma unroll
-      for (int k = 0; k < ADWIN_TOP_MAX / 32; ++k) {
-        const int j = lane + 32 * k;
-        if (j >= p.K || l.id[j] < 0) continue;
-        const float g = listed_grad(t, z[k], lq[k], p.forward);
-        gsq_listed = fmaf(g, g, gsq_listed);
-      }
-      gsq_listed = lane_sum(gsq_listed);
-    }
     return t;
   }
 
-  // The warp beside the sweeps.
-  __device__ __forceinline__ void extra_warp() {
-    for (int i = 0;; ++i) {
-      const RowInfo& info = sh.info[i & 3];
-      if (!info.row) break;
-      const TopList<TH>& l = sh.lists[i % 3];
-      const int64_t e = edge_of(info);
-      const float z = e >= 0 ? Elem<TIn>::load1(info.row, e) : -INFINITY;
-      const int j = e >= 0 ? listed(l, e) : -1;
-      {
-        const float zr = j >= 0 ? -INFINITY : z, m = fmaxf(warp_max(zr), kLowest), x = exp_below(zr, m);
-        publish(i & 1, m, lane_sum(x), lane_sum(x * x));
+  __device__ __forceinline__ void write_outputs(const RowInfo& info, const TopList& l, const TopScalars& t) const {
+    const int y = info.y;
+    const bool y_valid = y >= 0 && (int64_t)y < p.V;
+    int jy = ADWIN_TOP_MAX;
+    float gl = 0.f;
+    for (int k = lane; k < p.K; k += 32) {
+      if (!l.counts[k]) continue;
+      if (l.id[k] == y) jy = k;
+      if (p.gsq) {
+        const float g = listed_grad(t, l.z[k], l.lq[k], p.forward);
+        gl = fmaf(g, g, gl);
       }
-      meet();
-      float gl;
-      const TopScalars t = scalars(i & 1, l, gl);
-      if (info.out && e >= 0) {
-        const float g = j >= 0 ? listed_grad(t, z, l.lq[j], p.forward) : t.c_rest * exp_below(z, t.m_rest);
-        Elem<TOut>::store1(info.out, e, p.alpha * g);
-      }
-      if (me == 0) {
-        const int y = info.y;
-        const bool y_valid = y >= 0 && (int64_t)y < p.V;
-        int jy = -1;
-        for (int k = lane; k < p.K; k += 32)
-          if (y_valid && l.id[k] == y) jy = k;
-        jy = __reduce_max_sync(0xffffffffu, jy);
-        if (lane == 0) {
-          const float lse = t.M + t.ln_s;
-          p.kl[info.r] = t.kl;
-          p.logratio[info.r] = !y_valid ? __int_as_float(0x7fc00000)
-                               : jy >= 0 ? ((l.z[jy] - t.M) - t.ln_s) - l.lq[jy] : t.d_rest;
-          if (p.gsq) p.gsq[info.r] = p.alpha * p.alpha * (t.gsq_rest + gl);
-          if (p.lse) p.lse[info.r] = lse;
-          int bits = 0;
-          if (!y_valid) bits |= ADWIN_DEV_TOKEN_RANGE;
-          if (!isfinite(lse) || !isfinite(t.kl)) bits |= ADWIN_DEV_NONFINITE;
-          if (bits) atomicOr(p.status, bits);
-        }
-      }
-      look_up(i + 3);
-      prepare(i + 2);
+    }
+    jy = __reduce_min_sync(0xffffffffu, jy);
+    gl = lane_sum(gl);
+    if (lane == 0) {
+      const float lse = t.M + t.ln_s;
+      p.kl[info.r] = t.kl;
+      p.logratio[info.r] = !y_valid ? __int_as_float(0x7fc00000)
+                           : jy < ADWIN_TOP_MAX ? ((l.z[jy] - t.M) - t.ln_s) - l.lq[jy] : t.d_rest;
+      if (p.gsq) p.gsq[info.r] = p.alpha * p.alpha * (t.gsq_rest + gl);
+      if (p.lse) p.lse[info.r] = lse;
+      int bits = 0;
+      if (!y_valid) bits |= ADWIN_DEV_TOKEN_RANGE;
+      if (!isfinite(lse) || !isfinite(t.kl)) bits |= ADWIN_DEV_NONFINITE;
+      if (bits) atomicOr(p.status, bits);
     }
   }
 
-  // Asks for slot j of the row of `info`; position q of the ring.
-  __device__ __forceinline__ void fetch(const RowInfo& info, int j, int pos) const {
-    const int piece = j * TH + tid;
-    if (info.row && piece < info.np &&
-        ADWIN_CHK(pos >= 0 && pos < p.ring && info.entry0 + (int64_t)(piece + 1) * N <= p.V, p.status))
-      copy16(ring + (uint32_t)(pos * TH + tid) * 16u, info.row + (size_t)info.entry0 * sizeof(TIn) + (size_t)piece * 16);
-    copies_commit();
+  __device__ __forceinline__ void row_warp() {
+    TIn* const type = nullptr;
+    Cursor c = {(int64_t)(blockIdx.x / C), sh.list.count(p.range), (int64_t)(gridDim.x / C), 0};
+    for (int o = 0; o < 4; ++o) look_up(o, c);
+    __syncthreads();   // the lists may be prepared
+    uint32_t z_here = edge_logit(0), z_next = edge_logit(1);
+    meet();            // (the CTAs of a cluster are all there before anything is written to one)
+    for (int i = 0;; ++i) {
+      const RowInfo& info = info_of(i);
+      if (!info.row) break;
+      const TopList& l = sh.lists[i % 3];
+      const int e = edge_of(info), j = listed(l, e);
+      const float z = e >= 0 ? logit_of(z_here, type) : -INFINITY;
+      {
+        const float x = j >= 0 ? -INFINITY : z, m = fmaxf(warp_max(x), kLowest), w = exp_below(x, m);
+        publish(i & 1, m, lane_sum(w), lane_sum(w * w));
+      }
+      look_up(i + 4, c);
+      meet();
+      {
+        const TopScalars s = make_scalars(i & 1, l);
+        if (lane == 0) sh.scalars = s;
+      }
+      __syncthreads();
+      const TopScalars t = sh.scalars;
+      if (info.out && e >= 0)
+        Elem<TOut>::store1(info.out, e, p.alpha * (j >= 0 ? listed_grad(t, z, l.lq[j], p.forward)
+                                                          : t.c_rest * exp_below(z, t.m_rest)));
+      if (me == 0) write_outputs(info, l, t);
+      z_here = z_next;
+      z_next = edge_logit(i + 2);
+    }
+  }
+
+  // ------------------------------------------------------------------ the lists' warp
+  // Step 1: a row's list is asked for.
+  struct Asked {
+    int32_t id[kPerLane];
+    float lq[kPerLane], rest;
+  };
+  __device__ __forceinline__ void ask(int o, Asked& a) const {
+    const RowInfo& i = info_of(o);
+    const int64_t r = i.row ? i.r : -1;
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+      const int j = lane + 32 * k;
+      a.id[k] = -1;
+      a.lq[k] = 0.f;
+      if (r >= 0 && j < p.K) {
+        a.id[k] = __ldg(p.top_ids + r * p.K + j);
+        a.lq[k] = __ldg(p.top_logprobs + r * p.K + j);
+      }
+    }
+    a.rest = r >= 0 && p.rest ? __ldg(p.rest + r) : 0.f;
+  }
+  // Step 2: so are its logits.
+  struct Gathered {
+    Asked a;
+    uint32_t z[kPerLane];
+  };
+  __device__ __forceinline__ void gather(int o, const Asked& a, Gathered& g) const {
+    const char* row = info_of(o).row;
+    g.a = a;
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+      if (g.a.id[k] < -1 || (int64_t)g.a.id[k] >= p.V) {
+        if (me == 0) atomicOr(p.status, (int32_t)ADWIN_DEV_TOKEN_RANGE);
+        g.a.id[k] = -1;
+      }
+      g.z[k] = 0u;
+      if (g.a.id[k] >= 0) g.z[k] = raw_logit(row, g.a.id[k], static_cast<TIn*>(nullptr));
+    }
+  }
+  // Step 3: its chains and sums, into lists[o % 3].
+  __device__ __forceinline__ void prepare(int o, const Gathered& g) {
+    TopList& l = sh.lists[o % 3];
+    const RowInfo& i = info_of(o);
+    for (int k = lane; k < kChains; k += 32) l.first[k] = -1;
+    __syncwarp();
+    int chain[kPerLane];
+    float z[kPerLane];
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+      const int j = lane + 32 * k;
+      const int32_t id = g.a.id[k];
+      z[k] = logit_of(g.z[k], static_cast<TIn*>(nullptr));
+      chain[k] = id & (kChains - 1);
+      if (j >= p.K) continue;
+      int owner = -1, slot = -1;
+      const int e = id - i.entry0;
+      if (id >= 0 && e >= 0 && e < i.np * N) {
+        const uint32_t piece = (uint32_t)e / N;
+        owner = (int)(piece % TH);
+        slot = (int)(piece / TH);
+        chain[k] = owner & (kChains - 1);
+      }
+      l.id[j] = id;
+      l.lq[j] = g.a.lq[k];
+      l.z[j] = z[k];
+      l.slot[j] = slot;
+      l.owner[j] = (int16_t)owner;
+      if (id >= 0) l.next[j] = (int16_t)atomicExch(&l.first[chain[k]], j);   // (the order of a chain does not matter)
+    }
+    __syncwarp();
+    float zmax = kLowest;
+    bool counts[kPerLane];
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+      const int j = lane + 32 * k;
+      const int32_t id = g.a.id[k];
+      counts[k] = id >= 0;
+      if (id >= 0) {      // an index that the list has already does not count
+        for (int x = l.first[chain[k]]; x >= 0; x = l.next[x])
+          if (x < j && l.id[x] == id) counts[k] = false;
+        if (!counts[k] && me == 0) atomicOr(p.status, (int32_t)ADWIN_DEV_TOKEN_RANGE);
+      }
+      if (j < p.K) l.counts[j] = counts[k];
+      if (counts[k]) zmax = fmaxf(zmax, z[k]);
+    }
+    zmax = warp_max(zmax);
+    float s = 0.f, a = 0.f, q = 0.f;
+    double mass = 0.0;
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+      if (!counts[k]) continue;
+      const float lq = g.a.lq[k], e = exp_below(z[k], zmax), x = (z[k] - zmax) - lq, w = p.forward ? expf(lq) : e;
+      s += e;
+      if (p.forward) q += w;
+      a += w == 0.f ? 0.f : w * x;
+      if (!p.rest) mass += exp((double)lq);
+    }
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, x);
+      a += __shfl_xor_sync(0xffffffffu, a, x);
+      q += __shfl_xor_sync(0xffffffffu, q, x);
+      if (!p.rest) mass += __shfl_xor_sync(0xffffffffu, mass, x);
+    }
+    const float lqr = p.rest ? g.a.rest : (float)log(fmax(1.0 - mass, 5.9604644775390625e-8));   // 2^-24
+    if (lane == 0) {
+      l.lq_rest = lqr;
+      l.zmax = zmax;
+      l.s = s;
+      l.a = a;
+      l.q = q;
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ void list_warp() {
+    __syncthreads();
+    Asked asked;
+    Gathered got;
+    ask(0, asked);
+    gather(0, asked, got);
+    ask(1, asked);
+    prepare(0, got);
+    gather(1, asked, got);
+    ask(2, asked);
+    meet();
+    for (int i = 0; info_of(i).row; ++i) {
+      // beside the sums of row i: the list of the next, in a buffer that row i - 2 has left
+      prepare(i + 1, got);
+      gather(i + 2, asked, got);
+      ask(i + 3, asked);
+      meet();
+      __syncthreads();
+    }
+  }
+
+  // ------------------------------------------------------------------ the threads that sweep
+  // Which of this thread's slots (its pieces tid, tid + TH, ...) hold listed entries; with more than 32, which may.
+  __device__ __forceinline__ uint32_t marks(const TopList& l) const {
+    uint32_t m = 0;
+    for (int k = l.first[tid & (kChains - 1)]; k >= 0; k = l.next[k])
+      if (l.owner[k] == tid) m |= 1u << (l.slot[k] & 31);
+    return m;
   }
 
   __device__ __forceinline__ void sweeps() {
-    const int n = p.n, R = p.ring;
-    int base = 0;   // ring position of the row's slot 0
-    if (!STREAM) {
-      for (int q = 0; q < R; ++q) fetch(sh.info[q / n], q % n, q);   // (R <= 2 n)
-    }
+    const uint64_t keep = keep_policy(), drop = drop_policy();
+    __syncthreads();
+    meet();
     for (int i = 0;; ++i) {
-      const RowInfo& info = sh.info[i & 3];
+      const RowInfo& info = info_of(i);
       if (!info.row) break;
-      const TopList<TH>& l = sh.lists[i % 3];
-      const int np = info.np;
-      const uint4* src = reinterpret_cast<const uint4*>(info.row + (size_t)info.entry0 * sizeof(TIn));
-      const int slots = STREAM ? (np + TH - 1) / TH : n;
-      // which of this thread's slots hold listed entries (with more than 32 slots, which may)
-      const int chain = l.first[tid];
-      uint32_t marked = 0;
-      for (int j = chain; j >= 0; j = l.next[j])
-        if (l.slot[j] >= 0) marked |= 1u << (l.slot[j] & 31);
-
-      auto take = [&](int j) {
-        const int piece = j * TH + tid;
-        if (j >= slots || piece >= np) return masked_piece<TIn>();
-        if (STREAM) return ADWIN_CHK(info.entry0 + (int64_t)(piece + 1) * N <= p.V, p.status)
-                               ? __ldcg(src + piece) : masked_piece<TIn>();
-        int pos = base + j;
-        if (pos >= R) pos -= R;
-        return read16(ring + (uint32_t)(pos * TH + tid) * 16u);
+      const TopList& l = sh.lists[i % 3];
+      const int entry0 = info.entry0, np = info.np;
+      char* out = info.out;
+      const uint4* src = reinterpret_cast<const uint4*>(info.row + (size_t)entry0 * sizeof(TIn));
+      const uint32_t marked = marks(l);
+      // Pieces j, j + TH, ... of this thread; those behind the slice are masked.
+      auto take = [&](int j, uint64_t policy, uint4 (&v)[kGroup]) {
+        if (j + (kGroup - 1) * TH < np) {
+#pragma unroll
+          for (int k = 0; k < kGroup; ++k)
+            if (ADWIN_CHK(entry0 + (int64_t)(j + k * TH + 1) * N <= p.V, p.status)) v[k] = read16(src + j + k * TH, policy);
+        } else {
+#pragma unroll
+          for (int k = 0; k < kGroup; ++k) {
+            v[k] = masked_piece<TIn>();
+            if (j + k * TH < np && ADWIN_CHK(entry0 + (int64_t)(j + k * TH + 1) * N <= p.V, p.status))
+              v[k] = read16(src + j + k * TH, policy);
+          }
+        }
       };
-
       RestSum acc;
       acc.reset();
-      for (int j0 = 0; j0 < slots; j0 += kGroup) {
-        // copies committed so far: those of i n + R slots
-        if (!STREAM) copies_wait(R - (j0 + kGroup < n ? j0 + kGroup : n));
+      const uint64_t first = out ? keep : drop;
+#pragma unroll 1
+      for (int j = tid, slot = 0; j < np; j += kGroup * TH, slot += kGroup) {
         uint4 v[kGroup];
+        take(j, first, v);
+        if (marked >> (slot & 31) & ((1u << kGroup) - 1)) {
+          for (int x = l.first[tid & (kChains - 1)]; x >= 0; x = l.next[x]) {
+            if (l.owner[x] != tid) continue;
+            const int at = l.slot[x] - slot, e = (l.id[x] - entry0) & (N - 1);
 #pragma unroll
-        for (int k = 0; k < kGroup; ++k) {
-          v[k] = take(j0 + k);
-          if (marked >> ((j0 + k) & 31) & 1) {
-            for (int j = chain; j >= 0; j = l.next[j])
-              if (l.slot[j] == j0 + k) mask_entry<TIn>(v[k], (int)((l.id[j] - info.entry0) % N));
+            for (int k = 0; k < kGroup; ++k)
+              if (at == k) mask_entry<TIn>(v[k], e);
           }
         }
         acc.raise(group_max(v, static_cast<TIn*>(nullptr)));
+        const f2_t neg_m = splat2(-acc.m);
 #pragma unroll
         for (int k = 0; k < kGroup; ++k) {
           f2_t z[NP];
           Pairs<TIn>::make(v[k], z);
 #pragma unroll
-          for (int x = 0; x < NP; ++x) acc.add(z[x]);
+          for (int x = 0; x < NP; ++x) acc.add(z[x], neg_m);
         }
       }
       {
         const float m = warp_max(acc.m), w = exp_below(acc.m, m);
-        publish(i & 1, m, lane_sum(w * hsum2(acc.S)), lane_sum(w * w * hsum2(acc.Q)));
+        float s = w * hsum2(acc.S), q = w * w * hsum2(acc.Q);
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) {
+          s += __shfl_xor_sync(0xffffffffu, s, x);
+          q += __shfl_xor_sync(0xffffffffu, q, x);
+        }
+        publish(i & 1, m, s, q);
       }
       meet();
-      float unused;
-      const TopScalars t = scalars(i & 1, l, unused);
-
-      char* out = info.out ? info.out + (size_t)info.entry0 * sizeof(TOut) : nullptr;
-      constexpr int kOutAlign = N * sizeof(TOut) < 16 ? (int)(N * sizeof(TOut)) : 16;
+      __syncthreads();     // the scalars are there
+      if (!out) continue;
+      out += (size_t)entry0 * sizeof(TOut);
+      constexpr int kOutPiece = N * (int)sizeof(TOut), kOutAlign = kOutPiece < 16 ? kOutPiece : 16;
       const bool wide = (reinterpret_cast<uintptr_t>(out) & (kOutAlign - 1)) == 0;
-      const f2_t neg_m = splat2(-t.m_rest), coef = splat2(p.alpha * t.c_rest);
-      for (int j = 0; j < slots; ++j) {
-        const int piece = j * TH + tid;
-        if (out && piece < np) {
-          const uint4 v = take(j);
+      const f2_t neg_m = splat2(-sh.scalars.m_rest), coef = splat2(p.alpha * sh.scalars.c_rest);
+#pragma unroll 1
+      for (int j = tid, slot = 0; j < np; j += kGroup * TH, slot += kGroup) {
+        uint4 v[kGroup];
+        take(j, drop, v);
+        const bool any = marked >> (slot & 31) & ((1u << kGroup) - 1);
+#pragma unroll
+        for (int k = 0; k < kGroup; ++k) {
+          if (j + k * TH >= np) break;
           f2_t z[NP], g[NP];
-          Pairs<TIn>::make(v, z);
+          Pairs<TIn>::make(v[k], z);
 #pragma unroll
           for (int x = 0; x < NP; ++x) g[x] = mul2(coef, ex2_2(mul2(add2(z[x], neg_m), splat2(kLog2e))));
-          if (marked >> (j & 31) & 1) {
-            for (int k = chain; k >= 0; k = l.next[k]) {
-              if (l.slot[k] != j) continue;
-              const int at = (int)((l.id[k] - info.entry0) % N);
-              const float gl = p.alpha * listed_grad(t, l.z[k], l.lq[k], p.forward);
+          if (any) {
+            for (int y = l.first[tid & (kChains - 1)]; y >= 0; y = l.next[y]) {
+              if (l.owner[y] != tid || l.slot[y] != slot + k || !l.counts[y]) continue;
+              const int e = (l.id[y] - entry0) & (N - 1);
+              const float gl = p.alpha * listed_grad(sh.scalars, l.z[y], l.lq[y], p.forward);
 #pragma unroll
               for (int x = 0; x < NP; ++x) {
                 float a, b;
                 upk2(g[x], a, b);
-                g[x] = pk2(at == 2 * x ? gl : a, at == 2 * x + 1 ? gl : b);
+                g[x] = pk2(e == 2 * x ? gl : a, e == 2 * x + 1 ? gl : b);
               }
             }
           }
+          char* o = out + (size_t)(j + k * TH) * kOutPiece;
           if (wide) {
-            store_pairs<TOut>(out + (size_t)piece * N * sizeof(TOut), g);
+            store_pairs<TOut>(o, g);
           } else {
 #pragma unroll
             for (int x = 0; x < NP; ++x) {
               float a, b;
               upk2(g[x], a, b);
-              Elem<TOut>::store1(out, (int64_t)piece * N + 2 * x, a);
-              Elem<TOut>::store1(out, (int64_t)piece * N + 2 * x + 1, b);
+              Elem<TOut>::store1(o, 2 * x, a);
+              Elem<TOut>::store1(o, 2 * x + 1, b);
             }
           }
         }
-        if (!STREAM) {
-          int o = i, jj = j + R;
-          while (jj >= n) {
-            jj -= n;
-            ++o;
-          }
-          int pos = base + j;
-          if (pos >= R) pos -= R;
-          fetch(sh.info[o & 3], jj, pos);
-        }
       }
-      base += n;
-      while (base >= R) base -= R;
     }
-    if (!STREAM) copies_wait(0);
   }
 };
 
-template <typename TIn, typename TOut, int TH, int CTAS, bool STREAM>
-__global__ void __launch_bounds__(TH + 32, CTAS) topk_kl_kernel(const TopkParams p) {
+template <typename TIn, typename TOut, int TH, int CTAS>
+__global__ void __launch_bounds__(TH + 64, CTAS) topk_kl_kernel(const TopkParams p) {
   chain();
   extern __shared__ __align__(16) uint8_t smem[];
   TopkShared<TH>& sh = *reinterpret_cast<TopkShared<TH>*>(smem);
@@ -558,63 +657,58 @@ __global__ void __launch_bounds__(TH + 32, CTAS) topk_kl_kernel(const TopkParams
     if (p.gsq) p.gsq[r] = 0.f;
     if (p.lse) p.lse[r] = 0.f;
   });
-  for (int j = tid; j < 3 * TH; j += blockDim.x) sh.lists[j / TH].first[j % TH] = -1;
-  for (int j = tid; j < 3 * ADWIN_TOP_MAX; j += blockDim.x) sh.lists[j / ADWIN_TOP_MAX].owner[j % ADWIN_TOP_MAX] = -1;
   __syncthreads();
-  TopkCta<TIn, TOut, TH, STREAM> cta = {p, sh, smem_u32(smem) + (uint32_t)((sizeof(TopkShared<TH>) + 15) & ~size_t(15)),
-                                        C, me, tid, tid & 31, warp, sh.list.count(p.range),
-                                        (int64_t)(blockIdx.x / C), (int64_t)(gridDim.x / C)};
-  if (warp == TH / 32) {
-    for (int o = 0; o < 3; ++o) cta.look_up(o);
-    cta.prepare(0);
-    cta.prepare(1);
-  }
-  cta.meet();   // (the CTAs of a cluster are all there before anything is written to one)
-  if (warp == TH / 32) cta.extra_warp(); else cta.sweeps();
+  TopkCta<TIn, TOut, TH> cta = {p, sh, C, me, tid, tid & 31, warp};
+  if (warp == TH / 32) cta.row_warp();
+  else if (warp == TH / 32 + 1) cta.list_warp();
+  else cta.sweeps();
   if (p.zero_tail && p.grad) {
     const RowRange w = {p.window, p.rollout, p.range.B, p.range.T};
     zero_rows_outside<TOut>(w, p.grad, p.ld_grad, p.V);
   }
 }
 
-template <typename TIn, typename TOut, int TH, int CTAS, bool STREAM>
+template <typename TIn, typename TOut, int TH, int CTAS>
 cudaError_t launch_plan(const TopkParams& p, int C, int64_t rows, int sm_count, cudaStream_t s) {
-  const size_t base = (sizeof(TopkShared<TH>) + 15) & ~size_t(15);
-  // a CTA's whole share, the same for every launch of this kernel
-  constexpr size_t share = (size_t)(228 * 1024 / CTAS - 1024) & ~size_t(15);
-  const size_t smem = STREAM ? base : base + (size_t)p.ring * TH * 16;
-  if (smem > share) return cudaErrorInvalidValue;
-  auto kernel = topk_kl_kernel<TIn, TOut, TH, CTAS, STREAM>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)share);
+  const size_t smem = sizeof(TopkShared<TH>);
+  auto kernel = topk_kl_kernel<TIn, TOut, TH, CTAS>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  int64_t clusters = (int64_t)sm_count * CTAS / C;
-  if (clusters > rows) clusters = rows;
-  return launch_chained(kernel, (unsigned)(clusters * C), TH + 32, smem, C, s, p);
+  // as many clusters as the GPU holds at a time: their CTAs go on from row to row
+  static std::atomic<int> held[4];
+  int log_c = 0;
+  while ((1 << log_c) < C) ++log_c;
+  int n = C == 1 ? sm_count * CTAS : held[log_c].load();
+  if (n == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(sm_count * CTAS / C * C));
+    cfg.blockDim = dim3(TH + 64);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = C;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+    if (e != cudaSuccess) return e;
+    if (n < 1) return cudaErrorInvalidConfiguration;
+    held[log_c].store(n);
+  }
+  const int64_t clusters = n < rows ? n : rows;
+  return launch_chained(kernel, (unsigned)(clusters * C), TH + 64, smem, C, s, p);
 }
 
 template <typename TIn, typename TOut>
-cudaError_t launch(TopkParams p, int64_t rows, int sm_count, cudaStream_t s) {
+cudaError_t launch(const TopkParams& p, int64_t rows, int sm_count, cudaStream_t s) {
   const int64_t pieces = (p.V + Elem<TIn>::N - 1) / Elem<TIn>::N;
-  auto room = [](size_t th, size_t ctas) {
-    const size_t base = (th == 128 ? sizeof(TopkShared<128>) : th == 256 ? sizeof(TopkShared<256>) : sizeof(TopkShared<512>));
-    return (int)((228 * 1024 / ctas - 1024 - 32 - base) / (th * 16));
-  };
-  // few rows: several CTAs to a row, as long as each has two slots to a thread
+  // few rows: several CTAs to a row, as long as each has two groups of pieces to a thread
   int C = 1;
   while (C < kMaxCtas && rows * C * 2 <= sm_count && pieces >= (int64_t)C * 2 * 1024) C *= 2;
-  auto fit = [&](int th, int ctas) {
-    p.n = (int)((pieces + C - 1) / C + th - 1) / th;
-    if (p.n < 1) p.n = 1;
-    p.ring = room(th, ctas) < 2 * p.n ? room(th, ctas) : 2 * p.n;
-    if (p.ring > 25) p.ring = 25;
-    // the ring must hold a row and keep some of the next in flight
-    return p.ring >= p.n + (p.n + 3) / 4;
-  };
-  if (fit(128, 6)) return launch_plan<TIn, TOut, 128, 6, false>(p, C, rows, sm_count, s);
-  if (fit(256, 3)) return launch_plan<TIn, TOut, 256, 3, false>(p, C, rows, sm_count, s);
-  for (; C <= kMaxCtas; C *= 2)
-    if (fit(512, 1)) return launch_plan<TIn, TOut, 512, 1, false>(p, C, rows, sm_count, s);
-  return launch_plan<TIn, TOut, 512, 1, true>(p, 1, rows, sm_count, s);
+  if (pieces / C < 1024) return launch_plan<TIn, TOut, 128, 6>(p, C, rows, sm_count, s);
+  if (pieces / C < 4096) return launch_plan<TIn, TOut, 256, 3>(p, C, rows, sm_count, s);
+  if (C == 1 && pieces > 8192) C = 2;
+  return launch_plan<TIn, TOut, 512, 2>(p, C, rows, sm_count, s);
 }
 
 }  // namespace
