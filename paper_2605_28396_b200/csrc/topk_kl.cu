@@ -13,16 +13,19 @@
 // A row is read from memory once: its second read comes while it is still in L2 (the first asks for it to be
 // kept, the second and the gradient's stores to go first; a CTA, or a cluster with a slice of the
 // row each, has one row at a time).  Several CTAs per SM fill one another's gaps between the sweeps.  The warps meet
-// twice a row: when its sums are complete (a cluster's CTAs too), and when one more warp has made the row's
-// scalars of them.  That warp also looks the rows up, sums the few entries beside the 16-byte
-// pieces and writes the outputs; another prepares the lists, in three steps a row apart (index,
-// logit, chains and sums), so that it never waits for its loads.
+// twice a row: when their sums are there, and when one more warp has made the row's scalars of
+// them.  In a cluster that warp alone exchanges the CTAs' sums: a cluster barrier would have every
+// thread wait for its gradient's stores.  It
+// also looks the rows up, sums the few entries beside the 16-byte pieces and writes the outputs;
+// another prepares the lists, in three steps a row apart (index, logit, chains and sums), so that
+// it never waits for its loads.
 #include <atomic>
 
 #include "adwin_common.cuh"
 #include "adwin_internal.h"
 #include "exp_sums.cuh"
 #include "row_list.cuh"
+#include "tc_pipeline.cuh"
 
 namespace adwin {
 namespace {
@@ -49,6 +52,7 @@ struct TopkParams {
   int64_t ld_grad;
   float *kl, *logratio, *gsq, *lse;   // gsq, lse: may be null
   int32_t* status;
+  uint64_t limit_ns;         // of the wait for the records
 };
 
 // What the threads have to know of a row.
@@ -100,7 +104,10 @@ struct TopkShared {
   RowInfo info[kInfos];
   TopList lists[3];
   TopScalars scalars;
-  SumRecord rec[2][kMaxCtas * kWarps];
+  SumRecord rec[2][kWarps];          // of the CTA's warps
+  SumRecord slice[2][kMaxCtas];      // of the cluster's CTAs
+  unsigned long long complete[2];    // mbarriers: so they are there
+  int abort;
 };
 static_assert(alignof(TopkShared<128>) == 16 && sizeof(SumRecord) == 16, "records are stored 16 bytes at a time");
 
@@ -189,17 +196,56 @@ struct TopkCta {
   TopkShared<TH>& sh;
   const int C, me, tid, lane, warp;
 
-  // Hands a warp's sum to every CTA of the cluster.
   __device__ __forceinline__ void publish(int par, float m, float s, float q) const {
-    SumRecord* mine = &sh.rec[par][me * kWarps + warp];
-    if (C == 1) {
-      if (lane == 0) *mine = SumRecord{m, s, q, 0.f};
-    } else if (lane < C) {
-      remote_store4(map_to_rank(smem_u32(mine), (uint32_t)lane), m, s, q, 0.f);
-    }
+    if (lane == 0) sh.rec[par][warp] = SumRecord{m, s, q, 0.f};
   }
-  __device__ __forceinline__ void meet() const {
-    if (C == 1) __syncthreads(); else cluster_sync_all();
+  // Sum of n records, in every lane (n <= 32).
+  __device__ __forceinline__ SumRecord sum_of(const SumRecord* r, int n) const {
+    SumRecord x = {kLowest, 0.f, 0.f, 0.f};
+    if (lane < n) x = r[lane];
+    const float m = warp_max(x.m), w = exp_below(x.m, m);
+    float s = w * x.s, q = w * w * x.q;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, o);
+      q += __shfl_xor_sync(0xffffffffu, q, o);
+    }
+    return SumRecord{m, s, q, 0.f};
+  }
+  // The row's warp: the sum over the row, or false: the other CTAs' did not come in time.  A record's
+  // place is free: its last content, two rows ago, was read before any CTA sent what this one needed to come here.
+  __device__ __forceinline__ bool row_sum(int i, SumRecord& x) const {
+    const int par = i & 1;
+    x = sum_of(sh.rec[par], kWarps);
+    if (C == 1) return true;
+    const uint32_t bar = smem_u32(&sh.complete[par]);
+    if (lane < C) {
+      remote_store4(map_to_rank(smem_u32(&sh.slice[par][me]), (uint32_t)lane), x.m, x.s, x.q, 0.f);
+      tc::bar_arrive_cluster(map_to_rank(bar, (uint32_t)lane));
+    }
+    const bool ok = __all_sync(0xffffffffu, wait_cluster(bar, (i >> 1) & 1));
+    if (ok) x = sum_of(sh.slice[par], C);
+    return ok;
+  }
+  // Waits for a phase of a barrier that the cluster's CTAs arrive on, and sees what they wrote before.
+  __device__ __forceinline__ bool wait_cluster(uint32_t bar, uint32_t parity) const {
+    const uint64_t t0 = tc::timer_ns();
+    for (;;) {
+#pragma unroll 1
+      for (int k = 0; k < 64; ++k) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (p.limit_ns < 16) return false;   // (diagnostic: what is not there right now has run out)
+      }
+      if (tc::timer_ns() - t0 > p.limit_ns) return false;
+    }
   }
   __device__ __forceinline__ const RowInfo& info_of(int o) const { return sh.info[o % kInfos]; }
 
@@ -268,23 +314,8 @@ struct TopkCta {
     return e >= 0 ? found : -1;
   }
 
-  __device__ __forceinline__ TopScalars make_scalars(int par, const TopList& l) const {
-    float m = kLowest;
-    const int n = C * kWarps;
-    for (int i = lane; i < n; i += 32) m = fmaxf(m, sh.rec[par][i].m);
-    m = warp_max(m);
-    float s = 0.f, q = 0.f;
-    for (int i = lane; i < n; i += 32) {
-      const SumRecord r = sh.rec[par][i];
-      const float w = exp_below(r.m, m);
-      s = fmaf(w, r.s, s);
-      q = fmaf(w * w, r.q, q);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      s += __shfl_xor_sync(0xffffffffu, s, o);
-      q += __shfl_xor_sync(0xffffffffu, q, o);
-    }
+  __device__ __forceinline__ TopScalars make_scalars(const SumRecord& x, const TopList& l) const {
+    const float m = x.m, s = x.s, q = x.q;
     const float zmax = l.zmax, le = l.s, la = l.a, lqs = l.q, lqr = l.lq_rest;
     TopScalars t;
     const float M = fmaxf(m, zmax), wr = exp_below(m, M), wt = exp_below(zmax, M);
@@ -352,7 +383,7 @@ struct TopkCta {
     for (int o = 0; o < 4; ++o) look_up(o, c);
     __syncthreads();   // the lists may be prepared
     uint32_t z_here = edge_logit(0), z_next = edge_logit(1);
-    meet();            // (the CTAs of a cluster are all there before anything is written to one)
+    __syncthreads();
     for (int i = 0;; ++i) {
       const RowInfo& info = info_of(i);
       if (!info.row) break;
@@ -364,12 +395,16 @@ struct TopkCta {
         publish(i & 1, m, lane_sum(w), lane_sum(w * w));
       }
       look_up(i + 4, c);
-      meet();
-      {
-        const TopScalars s = make_scalars(i & 1, l);
-        if (lane == 0) sh.scalars = s;
+      __syncthreads();   // the warps' sums are there
+      SumRecord x;
+      const bool there = row_sum(i, x);
+      const TopScalars s = make_scalars(x, l);
+      if (lane == 0) {
+        sh.scalars = s;
+        if (!there) sh.abort = 1;
       }
       __syncthreads();
+      if (!there) break;
       const TopScalars t = sh.scalars;
       if (info.out && e >= 0)
         Elem<TOut>::store1(info.out, e, p.alpha * (j >= 0 ? listed_grad(t, z, l.lq[j], p.forward)
@@ -504,14 +539,15 @@ struct TopkCta {
     prepare(0, got);
     gather(1, asked, got);
     ask(2, asked);
-    meet();
+    __syncthreads();
     for (int i = 0; info_of(i).row; ++i) {
       // beside the sums of row i: the list of the next, in a buffer that row i - 2 has left
       prepare(i + 1, got);
       gather(i + 2, asked, got);
       ask(i + 3, asked);
-      meet();
       __syncthreads();
+      __syncthreads();
+      if (*static_cast<volatile int*>(&sh.abort)) break;
     }
   }
 
@@ -527,7 +563,7 @@ struct TopkCta {
   __device__ __forceinline__ void sweeps() {
     const uint64_t keep = keep_policy(), drop = drop_policy();
     __syncthreads();
-    meet();
+    __syncthreads();
     for (int i = 0;; ++i) {
       const RowInfo& info = info_of(i);
       if (!info.row) break;
@@ -587,8 +623,9 @@ struct TopkCta {
         }
         publish(i & 1, m, s, q);
       }
-      meet();
-      __syncthreads();     // the scalars are there
+      __syncthreads();     // the row's warp makes the scalars
+      __syncthreads();
+      if (*static_cast<volatile int*>(&sh.abort)) break;
       if (!out) continue;
       out += (size_t)entry0 * sizeof(TOut);
       constexpr int kOutPiece = N * (int)sizeof(TOut), kOutAlign = kOutPiece < 16 ? kOutPiece : 16;
@@ -657,11 +694,20 @@ __global__ void __launch_bounds__(TH + 64, CTAS) topk_kl_kernel(const TopkParams
     if (p.gsq) p.gsq[r] = 0.f;
     if (p.lse) p.lse[r] = 0.f;
   });
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) tc::bar_init(smem_u32(&sh.complete[i]), (uint32_t)C);
+    sh.abort = 0;
+    tc::bar_init_fence();
+  }
   __syncthreads();
+  if (C > 1) cluster_sync_all();   // every CTA and its barriers are there before anything is sent to one
   TopkCta<TIn, TOut, TH> cta = {p, sh, C, me, tid, tid & 31, warp};
   if (warp == TH / 32) cta.row_warp();
   else if (warp == TH / 32 + 1) cta.list_warp();
   else cta.sweeps();
+  __syncthreads();
+  if (tid == 0 && sh.abort) atomicOr(p.status, (int32_t)ADWIN_DEV_TIMEOUT);
+  if (C > 1) cluster_sync_all();   // none leaves while another may still send to it
   if (p.zero_tail && p.grad) {
     const RowRange w = {p.window, p.rollout, p.range.B, p.range.T};
     zero_rows_outside<TOut>(w, p.grad, p.ld_grad, p.V);
@@ -705,9 +751,15 @@ cudaError_t launch(const TopkParams& p, int64_t rows, int sm_count, cudaStream_t
   // few rows: several CTAs to a row, as long as each has two groups of pieces to a thread
   int C = 1;
   while (C < kMaxCtas && rows * C * 2 <= sm_count && pieces >= (int64_t)C * 2 * 1024) C *= 2;
-  if (pieces / C < 1024) return launch_plan<TIn, TOut, 128, 6>(p, C, rows, sm_count, s);
-  if (pieces / C < 4096) return launch_plan<TIn, TOut, 256, 3>(p, C, rows, sm_count, s);
-  if (C == 1 && pieces > 8192) C = 2;
+  // Many: as many threads to a row as leave its shorter half a group of pieces each, 32 warps per SM in all; and not
+  // many more than 45 MB of rows at a time, or their second read misses L2 (bf16, us for 128 threads x 8
+  // CTAs per SM / 256 x 4 / 512 x 2 / 512 x 2 in pairs: 18 432 rows of 4 096 entries 284 / 369 / 552 / -,
+  // 2 560 of 32 000 161 / 155 / 164 / 208, 2 300 of 50 257 131 / 118 / 121 / 149, 5 120 of 151 936
+  // - / - / 735 / 720).
+  const bool few = rows * C <= sm_count;
+  if (pieces / C < (few ? 1024 : 3000)) return launch_plan<TIn, TOut, 128, 8>(p, C, rows, sm_count, s);
+  if (pieces / C < (few ? 4096 : 8192)) return launch_plan<TIn, TOut, 256, 4>(p, C, rows, sm_count, s);
+  if (C == 1) C = 2;
   return launch_plan<TIn, TOut, 512, 2>(p, C, rows, sm_count, s);
 }
 
@@ -741,6 +793,7 @@ cudaError_t launch_topk_kl(const void* logits, int dtype, int64_t B, int64_t T, 
   p.gsq = gsq;
   p.lse = lse;
   p.status = status;
+  p.limit_ns = handshake_wait_limit_ns();
   const int64_t rows = B * T;
   const bool out_bf = grad && grad_dtype == ADWIN_BF16;
   if (dtype == ADWIN_BF16)
