@@ -4,10 +4,15 @@
 // quantize_rows_kernel:  step = max|x| / 127,  q = x / step to the nearest whole number, ties to even,
 // both divisions correctly rounded in fp32, so that every implementation of this definition gets the same q.
 //
+// linear_i8_few_kernel (up to 16 rows of x): one pass over w, memory-bound; see there.
+//
 // linear_i8_kernel: tcgen05.mma kind::i8 on CTA pairs, 256 x 256 tiles, accumulators of 32-bit whole numbers
 // in tensor memory (exact: d < 2^17 keeps every sum below 2^31), operands by TMA in the 128-byte
 // swizzle, 128 entries of the contraction a k-block.  The pipeline is that of tc_pipeline.cuh: bytes
 // are laid out as for 64 bf16.  An accumulator becomes float(acc) * (step_x * step_w): three roundings.
+// 4 096 x 2 560 against 151 936 channels: 1.23 ms (2.58 PFLOP/s; the tensor pipe is busy 72 % of the time, then the
+// power limit).  Rows of out that start off 16-byte boundaries leave through shared memory, a row of 32 results at a
+// time (777 x 1 000 against 50 257 channels, fp32 out: 294 us with scattered 4-byte stores, 114 so).
 #include <cuda_bf16.h>
 
 #include "adwin_common.cuh"
@@ -111,9 +116,15 @@ struct LinearParams {
   const float *step_x, *step_w;
   void* out;
   int64_t ldo;
+  bool whole;          // rows of out start on 16-byte boundaries
   int32_t* status;
   uint64_t limit_ns;
 };
+// Behind the stages: 32 x 32 results per epilogue warp on their way into rows of out that start anywhere.
+constexpr int kTurnPitch = 33;
+constexpr int kTurnBytes = 32 * kTurnPitch * 4;
+constexpr int kLinearSmem = kSmemBytes + (kEpiThreads / 32) * kTurnBytes;
+static_assert(kLinearSmem <= 227 * 1024, "shared memory");
 
 // Tile t: groups of kGroupM row tiles, within one the row tiles of a column tile follow one another, so
 // that W passes through once a group and the group's rows of x stay in L2.
@@ -212,40 +223,54 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       const int64_t n0 = (int64_t)nt * kBN + half * 128;
       const float sx = m < p.M ? p.step_x[m] : 0.f;
       TOut* o = static_cast<TOut*>(p.out) + (m < p.M ? m : 0) * p.ldo + n0;
-      const bool wide = (reinterpret_cast<uintptr_t>(o) & 15) == 0;
       if (!__all_sync(0xffffffffu, bar_wait(smem_addr(&ctrl->acc_full[slot]), aph, abort, p.limit_ns))) break;
       tc_fence_after_sync();
       const uint32_t t_lane = tmem_base + ((uint32_t)(quad * 32) << 16) + slot * kBN + (uint32_t)(half * 128);
+      float* turn = reinterpret_cast<float*>(smem_raw + (stage0 - smem_addr(smem_raw)) + kPairStages * kPairStageBytes) +
+                    (warp - kEpiWarp0) * (kTurnBytes / 4);
 #pragma unroll 1
       for (int j = 0; j < 4; ++j) {
-        uint32_t r[32];
-        __syncwarp();   // (lanes without a row come back here: the load is the warp's)
-        tmem_ld32(t_lane + j * 32, r);
-        tmem_ld_wait();
         const int64_t nj = n0 + j * 32;
         const int left = nj >= p.N ? 0 : (p.N - nj < 32 ? (int)(p.N - nj) : 32);
-        if (m >= p.M || left == 0) continue;
-        float v[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-          v[i] = (float)(int)r[i] * (sx * (i < left ? __ldg(p.step_w + nj + i) : 0.f));
+        if (left == 0) break;
+        uint32_t r[32];
+        __syncwarp();   // (the load is the warp's)
+        tmem_ld32(t_lane + j * 32, r);
+        tmem_ld_wait();
         TOut* oj = o + j * 32;
-        if (wide && left == 32) {
-          if (sizeof(TOut) == 2) {
+        if (p.whole && left == 32) {
+          if (m < p.M) {
+            float v[32];
 #pragma unroll
-            for (int i = 0; i < 32; i += 8)
-              *reinterpret_cast<uint4*>(oj + i) =
-                  make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
-                             pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
-          } else {
+            for (int i = 0; i < 32; ++i) v[i] = (float)(int)r[i] * (sx * __ldg(p.step_w + nj + i));
+            if (sizeof(TOut) == 2) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4)
-              *reinterpret_cast<float4*>(oj + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+              for (int i = 0; i < 32; i += 8)
+                *reinterpret_cast<uint4*>(oj + i) =
+                    make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
+                               pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; i += 4)
+                *reinterpret_cast<float4*>(oj + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+            }
           }
         } else {
+          // a lane holds a row's 32 results; turned over in shared memory it holds a column's, and a row goes out
+          // in one piece wherever it starts
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (i < left) Elem<TOut>::store1(oj, i, v[i]);
+          for (int i = 0; i < 32; ++i) turn[lane * kTurnPitch + i] = (float)(int)r[i];
+          __syncwarp();
+          const int64_t m0 = m - lane;
+          const int rows = p.M - m0 < 32 ? (p.M > m0 ? (int)(p.M - m0) : 0) : 32;
+          const float sw = lane < left ? __ldg(p.step_w + nj + lane) : 0.f;
+          TOut* col = static_cast<TOut*>(p.out) + m0 * p.ldo + nj + lane;
+#pragma unroll 8
+          for (int i = 0; i < rows; ++i) {
+            const float s = __shfl_sync(0xffffffffu, sx, i);
+            if (lane < left) Elem<TOut>::store1(col + i * p.ldo, 0, turn[i * kTurnPitch + lane] * (s * sw));
+          }
+          __syncwarp();
         }
       }
       tc_fence_before_sync();
@@ -266,6 +291,136 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
   }
 }
 
+// ---------------------------------------------------------------------------- few rows of x
+// Up to 16 tokens (decoding): W passes through once and bounds the call, and tensor-memory tiles would be
+// nearly empty.  Four warps take 16 rows of W, a quarter of the contraction each, straight from global memory into
+// the operand registers of mma.sync (any order of the contraction will do, as long as both operands have it:
+// a thread's 16 bytes of a row are its share of two instructions); x lies in shared memory.
+constexpr int kFewThreads = 512, kFewCtas = 2;
+constexpr int kFewGroups = kFewThreads / 128;
+constexpr int kFewMax = 16;          // tokens
+constexpr int kFewUnroll = 5;        // 64-byte blocks of a row in flight per warp, two loads each
+constexpr int kFewSmemX = 96 * 1024;
+
+struct FewParams {
+  const int8_t *x, *w;
+  int64_t ldx, ldw, N;
+  int M, d, pitch;     // pitch: bytes from row to row of x in shared memory, 64 more than a multiple of 128
+  const float *step_x, *step_w;
+  void* out;
+  int64_t ldo;
+  int32_t* status;
+};
+
+__device__ __forceinline__ void mma_i8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                       uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <typename TOut, int NT>   // NT: 8-token tiles
+__global__ void __launch_bounds__(kFewThreads, kFewCtas) linear_i8_few_kernel(const FewParams p) {
+  chain();
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  uint8_t* xs = smem_raw;
+  int* part = reinterpret_cast<int*>(smem_raw + NT * 8 * p.pitch);   // [group][parity][3][NT * 4][32]
+  const int tid = threadIdx.x, lane = tid & 31, group = tid >> 7, quarter = (tid >> 5) & 3;
+  const int pieces = p.pitch / 16;
+  for (int i = tid; i < NT * 8 * pieces; i += kFewThreads) {
+    const int row = i / pieces, k = (i % pieces) * 16;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (row < p.M && k < p.d) {
+      v = __ldg(reinterpret_cast<const uint4*>(p.x + (int64_t)row * p.ldx + k));
+      const int n = p.d - k;          // bytes behind the row's d count as zeros
+      uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n < 4 * j + 4) w[j] = n <= 4 * j ? 0u : w[j] & ((1u << (8 * (n - 4 * j))) - 1u);
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    *reinterpret_cast<uint4*>(xs + row * p.pitch + k) = v;
+  }
+  __syncthreads();
+  const int g = lane >> 2, t = lane & 3;
+  const int d16 = (p.d + 15) & ~15, blocks = (p.d + 63) / 64;
+  const uint8_t* xl = xs + g * p.pitch + t * 16;
+  const int64_t tiles = (p.N + 15) / 16, step = (int64_t)gridDim.x * kFewGroups;
+  int par = 0;
+  for (int64_t tile = (int64_t)blockIdx.x * kFewGroups + group; tile < tiles; tile += step, par ^= 1) {
+    const int64_t n0 = tile * 16 + g, n1 = n0 + 8;
+    const int8_t* w0 = p.w + (n0 < p.N ? n0 : p.N - 1) * p.ldw + t * 16;
+    const int8_t* w1 = p.w + (n1 < p.N ? n1 : p.N - 1) * p.ldw + t * 16;
+    int acc[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = 0;
+#pragma unroll 1
+    for (int kb = quarter; kb < blocks; kb += 4 * kFewUnroll) {
+      uint4 a[kFewUnroll], b[kFewUnroll];
+#pragma unroll
+      for (int u = 0; u < kFewUnroll; ++u) {
+        const int k = (kb + 4 * u) * 64;
+        a[u] = b[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (k + t * 16 < d16) {       // (a row's last bytes up to a multiple of 16 are there: its stride is one)
+          a[u] = __ldcs(reinterpret_cast<const uint4*>(w0 + k));
+          b[u] = __ldcs(reinterpret_cast<const uint4*>(w1 + k));
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kFewUnroll; ++u) {
+        const int k = (kb + 4 * u) * 64;
+        if (k >= p.d) break;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          const uint4 x = *reinterpret_cast<const uint4*>(xl + i * 8 * p.pitch + k);
+          mma_i8(acc[i], a[u].x, b[u].x, a[u].y, b[u].y, x.x, x.y);
+          mma_i8(acc[i], a[u].z, b[u].z, a[u].w, b[u].w, x.z, x.w);
+        }
+      }
+    }
+    int* mine = part + ((group * 2 + par) * 3) * (NT * 4 * 32) + lane;
+    if (quarter != 0) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mine[((quarter - 1) * NT * 4 + i * 4 + j) * 32] = acc[i][j];
+    }
+    asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory");
+    if (quarter == 0) {   // (the others go on; this buffer is written again after the next meeting)
+      const float s0 = n0 < p.N ? __ldg(p.step_w + n0) : 0.f, s1 = n1 < p.N ? __ldg(p.step_w + n1) : 0.f;
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          int v = acc[i][j];
+#pragma unroll
+          for (int q = 0; q < 3; ++q) v += mine[(q * NT * 4 + i * 4 + j) * 32];
+          const int m = i * 8 + t * 2 + (j & 1);
+          const int64_t n = j < 2 ? n0 : n1;
+          if (m < p.M && n < p.N)
+            Elem<TOut>::store1(p.out, m * p.ldo + n, (float)v * (__ldg(p.step_x + m) * (j < 2 ? s0 : s1)));
+        }
+      }
+    }
+  }
+}
+
+template <typename TOut, int NT>
+cudaError_t launch_few(const FewParams& p, int sm_count, cudaStream_t s) {
+  const size_t smem = (size_t)NT * 8 * p.pitch + (size_t)kFewGroups * 2 * 3 * NT * 4 * 32 * 4;
+  constexpr size_t limit = kFewSmemX + (size_t)kFewGroups * 2 * 3 * NT * 4 * 32 * 4;
+  const cudaError_t e = cudaFuncSetAttribute(linear_i8_few_kernel<TOut, NT>,
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)limit);
+  if (e != cudaSuccess) return e;
+  int64_t grid = (int64_t)sm_count * kFewCtas, tiles = ((p.N + 15) / 16 + kFewGroups - 1) / kFewGroups;
+  if (grid > tiles) grid = tiles;
+  return launch_chained(linear_i8_few_kernel<TOut, NT>, (unsigned)grid, kFewThreads, smem, 1, s, p);
+}
+
 }  // namespace
 
 cudaError_t launch_quantize_rows(const void* x, int dtype, int64_t M, int64_t d, int64_t ldx, int8_t* q,
@@ -281,6 +436,16 @@ cudaError_t launch_quantize_rows(const void* x, int dtype, int64_t M, int64_t d,
 cudaError_t launch_linear_i8(const int8_t* x, int64_t ldx, const float* step_x, const int8_t* w, int64_t ldw,
                              const float* step_w, int64_t M, int64_t N, int64_t d, void* out, int out_dtype,
                              int64_t ldo, int32_t* status, int sm_count, cudaStream_t s) {
+  // few tokens, d = 2 560 against 151 936 channels (389 MB: 59 us at the copy rate): 8 take 100 us on the tiles,
+  // 66 here, 16 98 and 75, 32 92 and 155
+  const int64_t row64 = (d + 63) / 64 * 64, pitch = row64 % 128 ? row64 : row64 + 64;
+  const int tiles8 = (int)((M + 7) / 8);
+  if (M <= kFewMax && tiles8 * 8 * pitch <= kFewSmemX) {
+    const FewParams f = {x, w, ldx, ldw, N, (int)M, (int)d, (int)pitch, step_x, step_w, out, ldo, status};
+    const bool bf = out_dtype == ADWIN_BF16;
+    if (tiles8 == 1) return bf ? launch_few<__nv_bfloat16, 1>(f, sm_count, s) : launch_few<float, 1>(f, sm_count, s);
+    return bf ? launch_few<__nv_bfloat16, 2>(f, sm_count, s) : launch_few<float, 2>(f, sm_count, s);
+  }
   LinearParams p = {};
   p.M = M;
   p.N = N;
@@ -291,12 +456,17 @@ cudaError_t launch_linear_i8(const int8_t* x, int64_t ldx, const float* step_x, 
   p.step_w = step_w;
   p.out = out;
   p.ldo = ldo;
+  p.whole = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && (ldo * (out_dtype == ADWIN_BF16 ? 2 : 4)) % 16 == 0;
   p.status = status;
   p.limit_ns = handshake_wait_limit_ns();
   CUtensorMap mx, mw;
   if (!make_map_i8(&mx, x, d, M, ldx, kBM) || !make_map_i8(&mw, w, d, N, ldw, kBM)) return cudaErrorInvalidValue;
-  return out_dtype == ADWIN_BF16 ? launch_pairs(linear_i8_kernel<__nv_bfloat16>, sm_count, s, mx, mw, p)
-                                 : launch_pairs(linear_i8_kernel<float>, sm_count, s, mx, mw, p);
+  auto launch = [&](auto kernel) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
+    if (e != cudaSuccess) return e;
+    return launch_chained(kernel, (unsigned)(sm_count & ~1), kThreads, kLinearSmem, 2, s, mx, mw, p);
+  };
+  return out_dtype == ADWIN_BF16 ? launch(linear_i8_kernel<__nv_bfloat16>) : launch(linear_i8_kernel<float>);
 }
 
 }  // namespace adwin
