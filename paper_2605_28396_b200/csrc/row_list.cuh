@@ -96,8 +96,8 @@ struct RowList {
 
 // Calls f(r) for the positions outside the processed ranges, spread over all threads of the grid.
 template <typename F>
-__device__ __forceinline__ void for_rows_outside(const RowRange& r, F f) {
-  if (!r.window && !r.rollout) return;
+__device__ __forceinline__ void for_rows_outside(const RowRange& r, const RowList& list, F f) {
+  if ((!r.window && !r.rollout) || (r.listed() && list.count(r) == r.B * r.T)) return;
   const int64_t rows = r.B * r.T, step = (int64_t)gridDim.x * blockDim.x;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows; i += step) {
     const int64_t b = i / r.T;

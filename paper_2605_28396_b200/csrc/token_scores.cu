@@ -34,6 +34,7 @@ constexpr int kUnroll = 8;       // 16-byte loads in flight per thread
 constexpr int kSlots = 12;       // units of a thread, at most
 constexpr int kCand = 384;       // entries that can be ranked at once
 constexpr int kMaxClusterX = 8;
+constexpr int kNone = (int)0x80000000;   // below every order_key
 // Order of floats as order of whole numbers, and back.
 __device__ __forceinline__ int order_key(float z) {
   const int b = __float_as_int(z + 0.f);
@@ -134,79 +135,108 @@ template <int TH>
 struct ScoreShared {
   RowList list;
   float red[3][TH / 32];
-  int count[2][TH / 32];
+  int2 count[2][TH / 32];
   int low[TH / 32], high[TH / 32];
   int n_cand;
   // alternatives
   float unit_sum[kSlots * TH];
   int unit_key[kSlots * TH];
   uint16_t open[kSlots * TH];
-  float cand_z[kCand];
-  int32_t cand_id[kCand];
+  unsigned long long cand[kCand];    // rank_key
+  int rank[kCand];
   float sorted_z[kCand];
   int32_t sorted_id[kCand];
+  Mass rest;
 };
-
-// Sum over the CTA of a whole number per thread, one barrier; consecutive calls alternate `flip`.
+// The CTA's shared memory.  The selection is not inlined (its registers would cost the sweep its own: 5 120 rows of
+// 151 936 entries 580 us inlined) and finds it by this name, not by a pointer that might lead anywhere.
+extern __shared__ __align__(16) uint8_t score_smem[];
 template <int TH>
-__device__ __forceinline__ int block_count(int v, int (&slots)[2][TH / 32], int& flip) {
-  v = __reduce_add_sync(0xffffffffu, v);
-  if ((threadIdx.x & 31) == 0) slots[flip][threadIdx.x >> 5] = v;
+__device__ __forceinline__ ScoreShared<TH>& score_shared() {
+  return *reinterpret_cast<ScoreShared<TH>*>(score_smem);
+}
+
+// Sums over the CTA of two whole numbers per thread, one barrier; consecutive calls alternate `flip`.
+template <int TH>
+__device__ __forceinline__ int2 block_count(int x, int y, int2 (&slots)[2][TH / 32], int& flip) {
+  x = __reduce_add_sync(0xffffffffu, x);
+  y = __reduce_add_sync(0xffffffffu, y);
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) slots[flip][threadIdx.x >> 5] = make_int2(x, y);
   __syncthreads();
-  int n = 0;
+  int2 v = make_int2(0, 0);
+  if (TH <= 128) {
 #pragma unroll
-  for (int w = 0; w < TH / 32; ++w) n += slots[flip][w];
+    for (int w = 0; w < TH / 32; ++w) {
+      v.x += slots[flip][w].x;
+      v.y += slots[flip][w].y;
+    }
+  } else {
+    if (lane < TH / 32) v = slots[flip][lane];
+    v.x = __reduce_add_sync(0xffffffffu, v.x);
+    v.y = __reduce_add_sync(0xffffffffu, v.y);
+  }
   flip ^= 1;
-  return n;
+  return v;
 }
 
 // Mass over the CTA of one per thread, in a fixed order; every thread returns it.
 template <int TH>
 __device__ __forceinline__ Mass block_mass(Mass v, float (&m)[TH / 32], float (&s)[TH / 32]) {
+  const int lane = threadIdx.x & 31;
   const float wm = warp_max(v.m);
   const float ws = lane_sum(ex2f(max_nan((v.m - wm) * kLog2e, kNil)) * v.s);
   __syncthreads();
-  if ((threadIdx.x & 31) == 0) {
+  if (lane == 0) {
     m[threadIdx.x >> 5] = wm;
     s[threadIdx.x >> 5] = ws;
   }
   __syncthreads();
-  Mass t = {kLowest, 0.f};
-#pragma unroll
-  for (int w = 0; w < TH / 32; ++w) t.add(m[w], s[w]);
+  const float lm = lane < TH / 32 ? m[lane] : kLowest, ls = lane < TH / 32 ? s[lane] : 0.f;
+  Mass t;
+  t.m = warp_max(lm);
+  t.s = lane_sum(ex2f(max_nan((lm - t.m) * kLog2e, kNil)) * ls);
   return t;
 }
+
+// Order of the alternatives as order of whole numbers: larger logits, then lower indices.
+__device__ __forceinline__ unsigned long long rank_key(float z, int32_t id) {
+  return ((unsigned long long)((uint32_t)order_key(z) ^ 0x80000000u) << 32) | (uint32_t)~id;
+}
+__device__ __forceinline__ float rank_logit(unsigned long long k) { return key_value((int)((uint32_t)(k >> 32) ^ 0x80000000u)); }
+__device__ __forceinline__ int32_t rank_id(unsigned long long k) { return (int32_t)~(uint32_t)k; }
 
 // A CTA's slice of a row.
 template <typename TIn>
 struct Slice {
   const char* row;
   const uint4* src;      // first piece of the slice
-  int64_t entry0;        // vocabulary index of its first entry
-  int64_t np;            // pieces
+  int entry0;            // vocabulary index of its first entry
+  int np;                // pieces
   int groups;            // groups of loads per unit
-  int64_t edge;          // an entry beside the pieces that this thread holds, or -1
+  int edge;              // an entry beside the pieces that this thread holds, or -1
   float edge_z;
 };
 
-// Walks the pieces of the opened units and this thread's edge entry: f(z, index) per entry.
+// Walks the pieces of the opened units: f(piece, index of its first entry).
 template <typename TIn, int TH, typename F>
 __device__ __forceinline__ void for_opened(const Slice<TIn>& s, const uint16_t* open, int n_open,
                                            int32_t* status, F f) {
   constexpr int N = Elem<TIn>::N;
   const int per = s.groups * kUnroll, total = n_open * per;
-  constexpr int kBatch = 4;
+  constexpr int kBatch = 1;
+#pragma unroll 1
   for (int i0 = threadIdx.x; i0 < total; i0 += kBatch * TH) {
     uint4 v[kBatch];
-    int64_t piece[kBatch];
+    int piece[kBatch];
 #pragma unroll
     for (int q = 0; q < kBatch; ++q) {
-      const int i = i0 + q * TH;
+      const uint32_t i = (uint32_t)(i0 + q * TH);
       piece[q] = -1;
-      if (i < total) {
-        const int u = open[i / per], w = i % per;
-        const int64_t p = ((int64_t)(u / TH) * s.groups + w / kUnroll) * (kUnroll * TH) +
-                          (w % kUnroll) * TH + (u % TH);
+      if (i < (uint32_t)total) {
+        const uint32_t nth = s.groups == 1 ? i / kUnroll : i / (uint32_t)per;
+        const int u = open[nth], w = (int)(i - nth * (uint32_t)per);
+        const int p = ((u / TH) * s.groups + w / kUnroll) * (kUnroll * TH) + (w % kUnroll) * TH + (u % TH);
         if (p < s.np && ADWIN_CHK(u < kSlots * TH, status)) {
           piece[q] = p;
           v[q] = __ldcg(s.src + p);
@@ -214,30 +244,113 @@ __device__ __forceinline__ void for_opened(const Slice<TIn>& s, const uint16_t* 
       }
     }
 #pragma unroll
-    for (int q = 0; q < kBatch; ++q) {
-      if (piece[q] < 0) continue;
-      float z[N];
-      Elem<TIn>::unpack(v[q], z);
-      const int64_t k0 = s.entry0 + piece[q] * N;
+    for (int q = 0; q < kBatch; ++q)
+      if (piece[q] >= 0) f(v[q], s.entry0 + piece[q] * N);
+  }
+}
+
+// A piece's entries at and above a threshold: one bit each; the others stay, these become -inf.
+__device__ __forceinline__ uint32_t split_piece(uint4& v, float from, __nv_bfloat16*) {
+  const __nv_bfloat162 f2 = __float2bfloat162_rn(from);   // (a threshold is a value of the logits' type, or below all of them)
+  uint32_t w[4] = {v.x, v.y, v.z, v.w}, bits = 0;
 #pragma unroll
-      for (int j = 0; j < N; ++j) f(z[j], k0 + j);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t m = __hge2_mask(reinterpret_cast<const __nv_bfloat162&>(w[i]), f2);
+    bits |= (m & (1u << (2 * i))) | (m & (2u << (2 * i + 16))) >> 16;
+    w[i] = (w[i] & ~m) | (0xff80ff80u & m);
+  }
+  v = make_uint4(w[0], w[1], w[2], w[3]);
+  return bits;
+}
+__device__ __forceinline__ uint32_t split_piece(uint4& v, float from, float*) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w}, bits = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool in = __uint_as_float(w[i]) >= from;
+    bits |= (in ? 1u : 0u) << i;
+    if (in) w[i] = 0xff800000u;
+  }
+  v = make_uint4(w[0], w[1], w[2], w[3]);
+  return bits;
+}
+template <typename TIn>
+__device__ __forceinline__ float piece_entry(const uint4& v, int e) {
+  if (sizeof(TIn) == 4) return __uint_as_float(e & 2 ? (e & 1 ? v.w : v.z) : (e & 1 ? v.y : v.x));
+  const uint32_t w = e & 4 ? (e & 2 ? v.w : v.z) : (e & 2 ? v.y : v.x);
+  return e & 1 ? bf16hi(w) : bf16lo(w);
+}
+
+// The entries of the opened units that belong to the list, where more reach tau than can be ranked: the K-th
+// largest value by bisection between tau and the largest, then the index up to which entries of that
+// value belong to it.  Returns their mass's complement in the opened units.
+template <typename TIn, int TH>
+__device__ __noinline__ Mass select_by_bisection(const Slice<TIn> s, int K, float M, int tau, int n, int n_open,
+                                                 int32_t* status) {
+  ScoreShared<TH>& sh = score_shared<TH>();
+  constexpr int N = Elem<TIn>::N;
+  int flip = 0;
+  __syncthreads();
+  auto walk = [&](auto f) {
+    for_opened<TIn, TH>(s, sh.open, n_open, status, [&](const uint4& v, int k0) {
+#pragma unroll 1
+      for (int e = 0; e < N; ++e) f(piece_entry<TIn>(v, e), k0 + e);
+    });
+    if (s.edge >= 0) f(s.edge_z, s.edge);
+  };
+  auto count = [&](float above, float equal, int upto) {
+    int v = 0;
+    walk([&](float z, int k) { v += (z >= above || (z >= equal && k <= upto)) ? 1 : 0; });
+    return block_count<TH>(v, 0, sh.count, flip).x;
+  };
+  int64_t lo = tau == kNone ? order_key(-INFINITY) : tau, hi = (int64_t)order_key(M) + 1;
+  int c = n;
+  while (hi - lo != 1 && c != K) {
+    const int64_t mid = lo + ((hi - lo) >> 1);
+    const int v = count(key_value((int)mid), INFINITY, -1);
+    if (v >= K) {
+      lo = mid;
+      c = v;
+    } else {
+      hi = mid;
     }
   }
-  if (s.edge >= 0) f(s.edge_z, s.edge);
+  const float equal = key_value((int)lo), above = c == K ? equal : key_value((int)hi);
+  int ilo = -1, ihi = s.entry0 + s.np * N + N;   // up to ilo: too few
+  if (c != K) {
+    while (ihi - ilo > 1) {
+      const int mid = ilo + (ihi - ilo) / 2;
+      if (count(above, equal, mid) >= K) ihi = mid; else ilo = mid;
+    }
+  }
+  if (threadIdx.x == 0) sh.n_cand = 0;
+  __syncthreads();
+  Mass below = {kLowest, 0.f};
+  walk([&](float z, int k) {
+    if (z >= above || (z >= equal && k <= ihi)) {
+      const int i = atomicAdd(&sh.n_cand, 1);
+      if (ADWIN_CHK(i < kCand, status)) {
+        sh.cand[i] = rank_key(z, k);
+        sh.rank[i] = 0;
+      }
+    } else {
+      below.add(z);
+    }
+  });
+  return below;
 }
 
 // The K largest entries of the slice into sh.sorted_z / sorted_id (fewer if it has fewer); returns their number and the
-// mass of all the others in `rest`.
+// mass of all the others in sh.rest.
 template <typename TIn, int TH>
-__device__ int select_top(ScoreShared<TH>& sh, const Slice<TIn>& s, int K, float M, int slots, int32_t* status,
-                          Mass& rest) {
+__device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int slots, int32_t* status) {
+  ScoreShared<TH>& sh = score_shared<TH>();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int flip = 0;
   // a thread reads back its own units only
-  int kmin = 0x7fffffff, kmax = (int)0x80000000, mine = 0;
+  int kmin = 0x7fffffff, kmax = kNone, mine = 0;
   for (int j = 0; j < slots; ++j) {
     const int k = sh.unit_key[j * TH + tid];
-    if (k == (int)0x80000000) continue;
+    if (k == kNone) continue;
     kmin = min(kmin, k);
     kmax = max(kmax, k);
     ++mine;
@@ -249,44 +362,47 @@ __device__ int select_top(ScoreShared<TH>& sh, const Slice<TIn>& s, int K, float
     sh.high[warp] = kmax;
   }
   if (tid == 0) sh.n_cand = 0;
-  const int units = block_count<TH>(mine, sh.count, flip);
-#pragma unroll
-  for (int w = 0; w < TH / 32; ++w) {
-    kmin = min(kmin, sh.low[w]);
-    kmax = max(kmax, sh.high[w]);
-  }
-  // tau: at least K units reach it, few more where the maxima differ
-  int tau = (int)0x80000000;
+  const int units = block_count<TH>(mine, 0, sh.count, flip).x;
+  kmin = __reduce_min_sync(0xffffffffu, lane < TH / 32 ? sh.low[lane] : 0x7fffffff);
+  kmax = __reduce_max_sync(0xffffffffu, lane < TH / 32 ? sh.high[lane] : kNone);
+  // tau: at least K units reach it, few more where the maxima differ.  Three thresholds a step.
+  int tau = kNone;
   if (units > K) {
     int64_t lo = kmin, hi = (int64_t)kmax + 1;
     int c = units;
     const int enough = K + K / 4 + 4;
     while (hi - lo != 1 && c > enough) {
-      const int64_t mid = lo + ((hi - lo) >> 1);
-      int v = 0;
-      for (int j = 0; j < slots; ++j) v += sh.unit_key[j * TH + tid] >= mid ? 1 : 0;
-      const int n = block_count<TH>(v, sh.count, flip);
-      if (n >= K) {
-        lo = mid;
-        c = n;
-      } else {
-        hi = mid;
+      const int64_t q = (hi - lo) >> 2, m2 = lo + ((hi - lo) >> 1), m1 = lo + (q > 0 ? q : 1), m3 = m2 + q;
+      int v1 = 0, v2 = 0, v3 = 0;
+      for (int j = 0; j < slots; ++j) {
+        const int k = sh.unit_key[j * TH + tid];
+        v1 += k >= m1 ? 1 : 0;
+        v2 += k >= m2 ? 1 : 0;
+        v3 += k >= m3 ? 1 : 0;
       }
+      const int2 n = block_count<TH>(v1 | (v2 << 16), v3, sh.count, flip);   // (at most kSlots TH each)
+      const int n1 = n.x & 0xffff, n2 = (int)((uint32_t)n.x >> 16), n3 = n.y;
+      if (n3 >= K) { lo = m3; c = n3; }
+      else if (n2 >= K) { lo = m2; c = n2; hi = m3 > m2 ? m3 : hi; }
+      else if (n1 >= K) { lo = m1; c = n1; hi = m2 > m1 ? m2 : hi; }
+      else hi = m1;
     }
     tau = (int)lo;
   }
-  const float tau_z = tau == (int)0x80000000 ? -INFINITY : key_value(tau);
+  // (for bf16 logits the next value of their type: no entry lies between)
+  float tau_z = tau == kNone ? -INFINITY : key_value(tau);
+  if (sizeof(TIn) == 2 && tau != kNone) {
+    const uint32_t bits = __float_as_uint(tau_z);
+    tau_z = __uint_as_float(bits & 0xffffu ? ((int)bits >= 0 ? (bits & 0xffff0000u) + 0x10000u : bits & 0xffff0000u) : bits);
+  }
   // the opened units, in an order of their own; the others' sums
   Mass others = {kLowest, 0.f};
   int n_mine = 0;
   for (int j = 0; j < slots; ++j) {
     const int k = sh.unit_key[j * TH + tid];
-    if (k == (int)0x80000000) continue;
-    if (k >= tau) {
-      ++n_mine;
-    } else {
-      others.add(fmaxf(key_value(k), kLowest), sh.unit_sum[j * TH + tid]);
-    }
+    if (k == kNone) continue;
+    if (k >= tau) ++n_mine;
+    else others.add(fmaxf(key_value(k), kLowest), sh.unit_sum[j * TH + tid]);
   }
   int before = n_mine;   // inclusive scan over the warp, then over the warps
 #pragma unroll
@@ -297,94 +413,95 @@ __device__ int select_top(ScoreShared<TH>& sh, const Slice<TIn>& s, int K, float
   __syncthreads();   // (every thread has read sh.low)
   if (lane == 31) sh.low[warp] = before;
   __syncthreads();
-  int n_open = 0, at = before - n_mine;
-#pragma unroll
-  for (int w = 0; w < TH / 32; ++w) {
-    if (w < warp) at += sh.low[w];
-    n_open += sh.low[w];
-  }
+  const int per_warp = lane < TH / 32 ? sh.low[lane] : 0;
+  const int n_open = __reduce_add_sync(0xffffffffu, per_warp);
+  int at = __reduce_add_sync(0xffffffffu, lane < warp ? per_warp : 0) + before - n_mine;
   for (int j = 0; j < slots; ++j) {
     const int k = sh.unit_key[j * TH + tid];
-    if (k != (int)0x80000000 && k >= tau) sh.open[at++] = (uint16_t)(j * TH + tid);
+    if (k != kNone && k >= tau) sh.open[at++] = (uint16_t)(j * TH + tid);
   }
   __syncthreads();
 
+  auto candidate = [&](float z, int k) {
+    const int i = atomicAdd(&sh.n_cand, 1);
+    if (i < kCand) {
+      sh.cand[i] = rank_key(z, k);
+      sh.rank[i] = 0;
+    }
+  };
+  // Entries below tau in the opened units: against the smallest of the units' maxima, where that is near enough
+  // (its unit is not opened, so what vanishes beside it is nothing to the mass outside)
   Mass below = {kLowest, 0.f};
-  for_opened<TIn, TH>(s, sh.open, n_open, status, [&](float z, int64_t k) {
-    if (z >= tau_z) {
-      const int i = atomicAdd(&sh.n_cand, 1);
-      if (i < kCand) {
-        sh.cand_z[i] = z;
-        sh.cand_id[i] = (int32_t)k;
-      }
+  const float ref = key_value(kmin);
+  const bool near = kmin < tau && ref >= tau_z - 60.f;
+  f2_t S = 0ull;
+  const f2_t neg_ref = splat2(-ref);
+  for_opened<TIn, TH>(s, sh.open, n_open, status, [&](uint4 v, int k0) {
+    const uint4 all = v;
+    uint32_t in = split_piece(v, tau_z, static_cast<TIn*>(nullptr));
+    while (in) {
+      const int e = __ffs((int)in) - 1;
+      in &= in - 1;
+      candidate(piece_entry<TIn>(all, e), k0 + e);
+    }
+    f2_t z[Pairs<TIn>::NP];
+    Pairs<TIn>::make(v, z);
+    if (near) {
+#pragma unroll
+      for (int j = 0; j < Pairs<TIn>::NP; ++j) S = add2(S, ex2_2(mul2(add2(z[j], neg_ref), splat2(kLog2e))));
     } else {
-      below.add(z);
+#pragma unroll
+      for (int j = 0; j < Pairs<TIn>::NP; ++j) {
+        float a, b;
+        upk2(z[j], a, b);
+        below.add(a);
+        below.add(b);
+      }
     }
   });
+  if (near) below = Mass{ref, hsum2(S)};
+  if (s.edge >= 0) {
+    if (s.edge_z >= tau_z) candidate(s.edge_z, s.edge);
+    else below.add(s.edge_z);
+  }
   __syncthreads();
   int n = sh.n_cand;
   if (n > kCand) {
-    // the K-th largest value by bisection between tau and the largest, then the index up to which
-    // entries of that value belong to the list
-    int64_t lo = tau == (int)0x80000000 ? order_key(-INFINITY) : tau, hi = (int64_t)order_key(M) + 1;
-    int c = n;
-    auto count = [&](float above, float equal, int64_t upto) {
-      int v = 0;
-      for_opened<TIn, TH>(s, sh.open, n_open, status, [&](float z, int64_t k) {
-        v += (z >= above || (z >= equal && k <= upto)) ? 1 : 0;
-      });
-      return block_count<TH>(v, sh.count, flip);
-    };
-    while (hi - lo != 1 && c != K) {
-      const int64_t mid = lo + ((hi - lo) >> 1);
-      const int v = count(key_value((int)mid), INFINITY, -1);
-      if (v >= K) {
-        lo = mid;
-        c = v;
-      } else {
-        hi = mid;
-      }
-    }
-    const float equal = key_value((int)lo), above = c == K ? equal : key_value((int)hi);
-    int64_t ilo = -1, ihi = s.entry0 + s.np * Elem<TIn>::N + Elem<TIn>::N;   // up to ilo: too few
-    if (c != K) {
-      while (ihi - ilo > 1) {
-        const int64_t mid = (ilo + ihi) >> 1;
-        if (count(above, equal, mid) >= K) ihi = mid; else ilo = mid;
-      }
-    }
-    if (tid == 0) sh.n_cand = 0;
-    __syncthreads();
-    below = Mass{kLowest, 0.f};
-    for_opened<TIn, TH>(s, sh.open, n_open, status, [&](float z, int64_t k) {
-      if (z >= above || (z >= equal && k <= ihi)) {
-        const int i = atomicAdd(&sh.n_cand, 1);
-        if (ADWIN_CHK(i < kCand, status)) {
-          sh.cand_z[i] = z;
-          sh.cand_id[i] = (int32_t)k;
-        }
-      } else {
-        below.add(z);
-      }
-    });
+    below = select_by_bisection<TIn, TH>(s, K, M, tau, n, n_open, status);
     __syncthreads();
     n = min(sh.n_cand, kCand);
   }
-  for (int i = tid; i < n; i += TH) {
-    const float z = sh.cand_z[i];
-    const int32_t id = sh.cand_id[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) {
-      const float x = sh.cand_z[j];
-      rank += (x > z || (x == z && sh.cand_id[j] < id)) ? 1 : 0;
+  // ranks: the candidates against one another, shared out over all threads
+  const int wide = (n + 31) & ~31, parts = wide <= TH ? TH / wide : 1;
+  if (parts > 1) {
+    const int i = tid % wide, part = tid / wide;
+    if (i < n && part < parts) {
+      const unsigned long long key = sh.cand[i];
+      int rank = 0;
+      for (int j = part; j < n; j += parts) rank += sh.cand[j] > key ? 1 : 0;
+      atomicAdd(&sh.rank[i], rank);
     }
-    sh.sorted_z[rank] = z;
-    sh.sorted_id[rank] = id;
+    __syncthreads();
+    if (tid < n) {
+      const unsigned long long key = sh.cand[tid];
+      sh.sorted_z[sh.rank[tid]] = rank_logit(key);
+      sh.sorted_id[sh.rank[tid]] = rank_id(key);
+    }
+  } else {
+    for (int i = tid; i < n; i += TH) {
+      const unsigned long long key = sh.cand[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += sh.cand[j] > key ? 1 : 0;
+      sh.sorted_z[rank] = rank_logit(key);
+      sh.sorted_id[rank] = rank_id(key);
+    }
   }
   __syncthreads();
   for (int i = K + tid; i < n; i += TH) below.add(sh.sorted_z[i]);
   below.add(others.m, others.s);
-  rest = block_mass<TH>(below, sh.red[0], sh.red[1]);
+  const Mass rest = block_mass<TH>(below, sh.red[0], sh.red[1]);
+  if (tid == 0) sh.rest = rest;
+  __syncthreads();
   return n < K ? n : K;
 }
 
@@ -397,19 +514,18 @@ __device__ __forceinline__ uint32_t cluster_size() {
 // TOP: alternatives are wanted.  Clusters: the CTAs of a cluster take a slice of the row each and
 // the first one joins their sums and lists.
 template <typename TIn, int TH, bool TOP>
-__global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(const ScoreParams p) {
+__global__ void __launch_bounds__(TH, TH == 128 ? (TOP ? 6 : 8) : 1) token_scores_kernel(const ScoreParams p) {
   chain();
-  extern __shared__ __align__(16) uint8_t smem[];
-  ScoreShared<TH>& sh = *reinterpret_cast<ScoreShared<TH>*>(smem);
+  ScoreShared<TH>& sh = score_shared<TH>();
   constexpr size_t kOwn = TOP ? sizeof(ScoreShared<TH>) : offsetof(ScoreShared<TH>, unit_sum);
-  SliceResult* slices = reinterpret_cast<SliceResult*>(smem + ((kOwn + 15) & ~size_t(15)));
+  SliceResult* slices = reinterpret_cast<SliceResult*>(score_smem + ((kOwn + 15) & ~size_t(15)));
   constexpr int N = Elem<TIn>::N;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = (int)cluster_size(), me = C > 1 ? (int)cluster_rank() : 0;
   const int K = TOP ? p.K : 0;
 
   sh.list.build(p.range, p.status);
-  for_rows_outside(p.range, [&](int64_t r) {
+  for_rows_outside(p.range, sh.list, [&](int64_t r) {
     p.logprob[r] = 0.f;
     if (p.entropy) p.entropy[r] = 0.f;
     if (p.lse) p.lse[r] = 0.f;
@@ -429,18 +545,18 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
     Slice<TIn> s;
     s.row = static_cast<const char*>(p.logits) + (size_t)r * p.ld * sizeof(TIn);
     const RowPieces rp = RowPieces::of<TIn>(s.row, p.V);
-    const int64_t per = (rp.pieces + C - 1) / C, first = per * me < rp.pieces ? per * me : rp.pieces;
-    s.np = first + per < rp.pieces ? per : rp.pieces - first;
+    const int pieces = (int)rp.pieces, per = C == 1 ? pieces : (int)((uint32_t)(pieces + C - 1) / (uint32_t)C);
+    const int first = per * me < pieces ? per * me : pieces;
+    s.np = first + per < pieces ? per : pieces - first;
     s.entry0 = rp.head + first * N;
     s.src = reinterpret_cast<const uint4*>(s.row + (size_t)s.entry0 * sizeof(TIn));
     s.edge = -1;
     if (me == 0 && tid < rp.head) s.edge = tid;
-    if (me == C - 1 && tid >= 32 && tid - 32 < rp.tail) s.edge = p.V - rp.tail + (tid - 32);
+    if (me == C - 1 && tid >= 32 && tid - 32 < rp.tail) s.edge = (int)p.V - rp.tail + (tid - 32);
     s.edge_z = s.edge >= 0 ? Elem<TIn>::load1(s.row, s.edge) : 0.f;
-    const int64_t trips = (s.np + kUnroll * TH - 1) / (kUnroll * TH);
-    s.groups = (int)((trips + kSlots - 1) / kSlots);
-    if (s.groups < 1) s.groups = 1;
-    const int slots = (int)((trips + s.groups - 1) / s.groups);
+    const int trips = (s.np + kUnroll * TH - 1) / (kUnroll * TH);
+    s.groups = trips <= kSlots ? 1 : (trips + kSlots - 1) / kSlots;
+    const int slots = s.groups == 1 ? trips : (trips + s.groups - 1) / s.groups;
     const int y = (me == 0 && tid == 0) ? p.tokens[r] : 0;
     const bool y_valid = y >= 0 && (int64_t)y < p.V;
     const float zy = (me == 0 && tid == 0 && y_valid) ? Elem<TIn>::load1(s.row, y) : 0.f;
@@ -453,24 +569,24 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
       acc.s = ex2f(t);
       acc.a = acc.s * t;
     }
-    int64_t i = tid;
+    int i = tid;
     for (int slot = 0; slot < slots; ++slot) {
       ExpSum unit;
       unit.reset();
-      int key = (int)0x80000000;
+      int key = kNone;
       for (int g = 0; g < s.groups; ++g, i += kUnroll * TH) {
         if (i - tid >= s.np) break;
         uint4 v[kUnroll];
         if (i - tid + kUnroll * TH <= s.np) {
 #pragma unroll
           for (int k = 0; k < kUnroll; ++k)
-            if (ADWIN_CHK(s.entry0 + (i + k * TH + 1) * N <= p.V, p.status)) v[k] = __ldcs(s.src + i + k * TH);
+            if (ADWIN_CHK(s.entry0 + (int64_t)(i + k * TH + 1) * N <= p.V, p.status)) v[k] = __ldcs(s.src + i + k * TH);
         } else {
           constexpr uint32_t kMasked = sizeof(TIn) == 2 ? 0xff80ff80u : 0xff800000u;   // -infinity
 #pragma unroll
           for (int k = 0; k < kUnroll; ++k) {
             v[k] = make_uint4(kMasked, kMasked, kMasked, kMasked);
-            if (i + k * TH < s.np && ADWIN_CHK(s.entry0 + (i + k * TH + 1) * N <= p.V, p.status))
+            if (i + k * TH < s.np && ADWIN_CHK(s.entry0 + (int64_t)(i + k * TH + 1) * N <= p.V, p.status))
               v[k] = __ldcs(s.src + i + k * TH);
           }
         }
@@ -496,25 +612,23 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
         sh.red[2][warp] = wa;
       }
       __syncthreads();
-      tot.reset();
-#pragma unroll
-      for (int q = 0; q < TH / 32; ++q) tot.m = fmaxf(tot.m, sh.red[0][q]);
-#pragma unroll
-      for (int q = 0; q < TH / 32; ++q) {
-        const float tq = max_nan((sh.red[0][q] - tot.m) * kLog2e, kNil), wq = ex2f(tq);
-        tot.s = fmaf(wq, sh.red[1][q], tot.s);
-        tot.a = fmaf(wq, fmaf(sh.red[1][q], tq, sh.red[2][q]), tot.a);
-      }
+      const bool there = lane < TH / 32;
+      const float lm = there ? sh.red[0][lane] : kLowest, ls = there ? sh.red[1][lane] : 0.f;
+      const float la = there ? sh.red[2][lane] : 0.f;
+      tot.m = warp_max(lm);
+      const float tq = max_nan((lm - tot.m) * kLog2e, kNil), wq = ex2f(tq);
+      tot.s = lane_sum(wq * ls);
+      tot.a = lane_sum(wq * fmaf(ls, tq, la));
     }
     // (a slice of masked entries only is no reason to stop, a NaN or +infinity is)
     const bool sound = isfinite(tot.s) && isfinite(tot.m);
     Mass rest = {kLowest, 0.f};
     int n_top = 0;
-    if (TOP && sound && (C > 1 || tot.s > 0.f))
-      n_top = select_top<TIn, TH>(sh, s, K, tot.m, slots, p.status, rest);
+    if (TOP && sound && (C > 1 || tot.s > 0.f)) {
+      n_top = select_top<TIn, TH>(s, K, tot.m, slots, p.status);
+      rest = sh.rest;
+    }
 
-    const float* list_z = TOP ? sh.sorted_z : nullptr;
-    const int32_t* list_id = TOP ? sh.sorted_id : nullptr;
     if (C > 1) {
       // hand the slice's result to the first CTA
       const uint32_t dst = map_to_rank(smem_u32(&slices[me]), 0);
@@ -530,15 +644,17 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
       }
       cluster_sync_all();
       if (me == 0) {
-        tot.reset();
-        for (int q = 0; q < C; ++q) tot.m = fmaxf(tot.m, slices[q].m);
-        rest = Mass{kLowest, 0.f};
-        for (int q = 0; q < C; ++q) {
-          const float tq = max_nan((slices[q].m - tot.m) * kLog2e, kNil), wq = ex2f(tq);
-          tot.s = fmaf(wq, slices[q].s, tot.s);
-          tot.a = fmaf(wq, fmaf(slices[q].s, tq, slices[q].a), tot.a);
-          rest.add(slices[q].rest.m, slices[q].rest.s);
-        }
+        const bool there = lane < C;
+        const float lm = there ? slices[lane].m : kLowest, ls = there ? slices[lane].s : 0.f;
+        const float la = there ? slices[lane].a : 0.f;
+        tot.m = warp_max(lm);
+        const float tq = max_nan((lm - tot.m) * kLog2e, kNil), wq = ex2f(tq);
+        tot.s = lane_sum(wq * ls);
+        tot.a = lane_sum(wq * fmaf(ls, tq, la));
+        Mass lr = {kLowest, 0.f};
+        if (there) lr = slices[lane].rest;
+        rest.m = warp_max(lr.m);
+        rest.s = lane_sum(ex2f(max_nan((lr.m - rest.m) * kLog2e, kNil)) * lr.s);
         if constexpr (TOP) {
           // rank of an entry: its place in its own list and, by bisection, in the others'; equal
           // entries of an earlier slice come first, they have the lower index
@@ -547,28 +663,34 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
             const int q = i2 / K, j = i2 % K;
             if (j >= slices[q].n) continue;
             const float z = slices[q].z[j];
-            int rank = j;
-            for (int o = 0; o < C; ++o) {
-              if (o == q) continue;
-              int lo = 0, hi = slices[o].n;
-              while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                const float x = slices[o].z[mid];
-                if (x > z || (x == z && o < q)) lo = mid + 1; else hi = mid;
-              }
-              rank += lo;
+            // (all searches at once: a step in each list, the first one whose entries come later)
+            int lo[kMaxClusterX], len[kMaxClusterX];
+#pragma unroll
+            for (int o = 0; o < kMaxClusterX; ++o) {
+              lo[o] = 0;
+              len[o] = o < C && o != q ? slices[o].n : 0;
             }
+            for (int width = ADWIN_TOP_MAX; width > 0; width >>= 1) {
+#pragma unroll
+              for (int o = 0; o < kMaxClusterX; ++o) {
+                const int at = lo[o] + width;
+                if (at > len[o]) continue;
+                const float x = slices[o].z[at - 1];
+                if (x > z || (x == z && o < q)) lo[o] = at;
+              }
+            }
+            int rank = j;
+#pragma unroll
+            for (int o = 0; o < kMaxClusterX; ++o) rank += lo[o];
             if (rank < K) {
-              sh.cand_z[rank] = z;
-              sh.cand_id[rank] = slices[q].id[j];
+              sh.sorted_z[rank] = z;
+              sh.sorted_id[rank] = slices[q].id[j];
             } else {
               losers.add(z);
             }
           }
           losers = block_mass<TH>(losers, sh.red[0], sh.red[1]);   // (its barriers publish the list)
           rest.add(losers.m, losers.s);
-          list_z = sh.cand_z;
-          list_id = sh.cand_id;
         }
       }
     }
@@ -578,8 +700,8 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
       const float nan = __int_as_float(0x7fc00000);
       if constexpr (TOP) {
         for (int j = tid; j < K; j += TH) {
-          p.top_ids[r * K + j] = finite ? list_id[j] : -1;
-          p.top_logprobs[r * K + j] = finite ? (list_z[j] - tot.m) - ln_s : nan;
+          p.top_ids[r * K + j] = finite ? sh.sorted_id[j] : -1;
+          p.top_logprobs[r * K + j] = finite ? (sh.sorted_z[j] - tot.m) - ln_s : nan;
         }
       }
       if (tid == 0) {

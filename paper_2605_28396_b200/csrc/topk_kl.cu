@@ -688,7 +688,7 @@ __global__ void __launch_bounds__(TH + 64, CTAS) topk_kl_kernel(const TopkParams
   if (p.window && !p.range.window && blockIdx.x == 0)
     for (int64_t b = tid; b < p.range.B; b += blockDim.x)
       if (p.window[b] < 0) atomicOr(p.status, (int32_t)ADWIN_DEV_WINDOW);
-  for_rows_outside(p.range, [&](int64_t r) {
+  for_rows_outside(p.range, sh.list, [&](int64_t r) {
     p.kl[r] = 0.f;
     p.logratio[r] = 0.f;
     if (p.gsq) p.gsq[r] = 0.f;
