@@ -11,7 +11,7 @@
 
 namespace adwin {
 
-constexpr int kListMax = 512;
+constexpr int kListMax = 256;
 
 struct RowRange {
   const int32_t* window;    // [B] or null (= T)

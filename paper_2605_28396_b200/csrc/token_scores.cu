@@ -32,7 +32,7 @@ namespace {
 
 constexpr int kUnroll = 8;       // 16-byte loads in flight per thread
 constexpr int kSlots = 12;       // units of a thread, at most
-constexpr int kCand = 384;       // entries that can be ranked at once
+constexpr int kCand = 256;       // entries that can be ranked at once
 constexpr int kMaxClusterX = 8;
 constexpr int kNone = (int)0x80000000;   // below every order_key
 // Order of floats as order of whole numbers, and back.
@@ -114,7 +114,7 @@ struct ScoreParams {
   int64_t V, ld;
   RowRange range;
   const int32_t* tokens;
-  int K;
+  int K, units;                     // units: room for those of a CTA's slice
   float *logprob, *entropy, *lse;   // entropy, lse: may be null
   int32_t* top_ids;
   float *top_logprobs, *rest;       // rest: may be null
@@ -139,14 +139,20 @@ struct ScoreShared {
   int low[TH / 32], high[TH / 32];
   int n_cand;
   // alternatives
-  float unit_sum[kSlots * TH];
-  int unit_key[kSlots * TH];
-  uint16_t open[kSlots * TH];
+  Mass rest;
   unsigned long long cand[kCand];    // rank_key
   int rank[kCand];
   float sorted_z[kCand];
   int32_t sorted_id[kCand];
-  Mass rest;
+};
+// The units of a row of `slots` to a thread follow: no more than the call's rows need, for shared memory is
+// taken from L1, where loads in flight wait (64 alternatives of 40 960 rows of 4 096 entries 1 037 us with room for 12 slots,
+// 638 with 8, 631 with the one they need).
+struct Units {
+  float* sum;       // of exponentials, against the unit's largest logit
+  int* key;         // order_key of that
+  uint16_t* open;   // units that may hold alternatives
+  static constexpr size_t kBytes = 10;   // per unit
 };
 // The CTA's shared memory.  The selection is not inlined (its registers would cost the sweep its own: 5 120 rows of
 // 151 936 entries 580 us inlined) and finds it by this name, not by a pointer that might lead anywhere.
@@ -154,6 +160,18 @@ extern __shared__ __align__(16) uint8_t score_smem[];
 template <int TH>
 __device__ __forceinline__ ScoreShared<TH>& score_shared() {
   return *reinterpret_cast<ScoreShared<TH>*>(score_smem);
+}
+template <int TH>
+__host__ __device__ constexpr size_t units_offset() {
+  return (sizeof(ScoreShared<TH>) + 15) & ~size_t(15);
+}
+template <int TH>
+__device__ __forceinline__ Units units_of(int capacity) {
+  Units u;
+  u.sum = reinterpret_cast<float*>(score_smem + units_offset<TH>());
+  u.key = reinterpret_cast<int*>(u.sum + capacity);
+  u.open = reinterpret_cast<uint16_t*>(u.key + capacity);
+  return u;
 }
 
 // Sums over the CTA of two whole numbers per thread, one barrier; consecutive calls alternate `flip`.
@@ -285,13 +303,14 @@ __device__ __forceinline__ float piece_entry(const uint4& v, int e) {
 // value belong to it.  Returns their mass's complement in the opened units.
 template <typename TIn, int TH>
 __device__ __noinline__ Mass select_by_bisection(const Slice<TIn> s, int K, float M, int tau, int n, int n_open,
-                                                 int32_t* status) {
+                                                 int room, int32_t* status) {
   ScoreShared<TH>& sh = score_shared<TH>();
+  const Units un = units_of<TH>(room);
   constexpr int N = Elem<TIn>::N;
   int flip = 0;
   __syncthreads();
   auto walk = [&](auto f) {
-    for_opened<TIn, TH>(s, sh.open, n_open, status, [&](const uint4& v, int k0) {
+    for_opened<TIn, TH>(s, un.open, n_open, status, [&](const uint4& v, int k0) {
 #pragma unroll 1
       for (int e = 0; e < N; ++e) f(piece_entry<TIn>(v, e), k0 + e);
     });
@@ -342,14 +361,15 @@ __device__ __noinline__ Mass select_by_bisection(const Slice<TIn> s, int K, floa
 // The K largest entries of the slice into sh.sorted_z / sorted_id (fewer if it has fewer); returns their number and the
 // mass of all the others in sh.rest.
 template <typename TIn, int TH>
-__device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int slots, int32_t* status) {
+__device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int slots, int room, int32_t* status) {
   ScoreShared<TH>& sh = score_shared<TH>();
+  const Units un = units_of<TH>(room);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int flip = 0;
   // a thread reads back its own units only
   int kmin = 0x7fffffff, kmax = kNone, mine = 0;
   for (int j = 0; j < slots; ++j) {
-    const int k = sh.unit_key[j * TH + tid];
+    const int k = un.key[j * TH + tid];
     if (k == kNone) continue;
     kmin = min(kmin, k);
     kmax = max(kmax, k);
@@ -375,7 +395,7 @@ __device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int s
       const int64_t q = (hi - lo) >> 2, m2 = lo + ((hi - lo) >> 1), m1 = lo + (q > 0 ? q : 1), m3 = m2 + q;
       int v1 = 0, v2 = 0, v3 = 0;
       for (int j = 0; j < slots; ++j) {
-        const int k = sh.unit_key[j * TH + tid];
+        const int k = un.key[j * TH + tid];
         v1 += k >= m1 ? 1 : 0;
         v2 += k >= m2 ? 1 : 0;
         v3 += k >= m3 ? 1 : 0;
@@ -399,10 +419,10 @@ __device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int s
   Mass others = {kLowest, 0.f};
   int n_mine = 0;
   for (int j = 0; j < slots; ++j) {
-    const int k = sh.unit_key[j * TH + tid];
+    const int k = un.key[j * TH + tid];
     if (k == kNone) continue;
     if (k >= tau) ++n_mine;
-    else others.add(fmaxf(key_value(k), kLowest), sh.unit_sum[j * TH + tid]);
+    else others.add(fmaxf(key_value(k), kLowest), un.sum[j * TH + tid]);
   }
   int before = n_mine;   // inclusive scan over the warp, then over the warps
 #pragma unroll
@@ -417,8 +437,8 @@ __device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int s
   const int n_open = __reduce_add_sync(0xffffffffu, per_warp);
   int at = __reduce_add_sync(0xffffffffu, lane < warp ? per_warp : 0) + before - n_mine;
   for (int j = 0; j < slots; ++j) {
-    const int k = sh.unit_key[j * TH + tid];
-    if (k != kNone && k >= tau) sh.open[at++] = (uint16_t)(j * TH + tid);
+    const int k = un.key[j * TH + tid];
+    if (k != kNone && k >= tau) un.open[at++] = (uint16_t)(j * TH + tid);
   }
   __syncthreads();
 
@@ -436,7 +456,7 @@ __device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int s
   const bool near = kmin < tau && ref >= tau_z - 60.f;
   f2_t S = 0ull;
   const f2_t neg_ref = splat2(-ref);
-  for_opened<TIn, TH>(s, sh.open, n_open, status, [&](uint4 v, int k0) {
+  for_opened<TIn, TH>(s, un.open, n_open, status, [&](uint4 v, int k0) {
     const uint4 all = v;
     uint32_t in = split_piece(v, tau_z, static_cast<TIn*>(nullptr));
     while (in) {
@@ -467,7 +487,7 @@ __device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int s
   __syncthreads();
   int n = sh.n_cand;
   if (n > kCand) {
-    below = select_by_bisection<TIn, TH>(s, K, M, tau, n, n_open, status);
+    below = select_by_bisection<TIn, TH>(s, K, M, tau, n, n_open, room, status);
     __syncthreads();
     n = min(sh.n_cand, kCand);
   }
@@ -514,11 +534,12 @@ __device__ __forceinline__ uint32_t cluster_size() {
 // TOP: alternatives are wanted.  Clusters: the CTAs of a cluster take a slice of the row each and
 // the first one joins their sums and lists.
 template <typename TIn, int TH, bool TOP>
-__global__ void __launch_bounds__(TH, TH == 128 ? (TOP ? 6 : 8) : 1) token_scores_kernel(const ScoreParams p) {
+__global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(const ScoreParams p) {
   chain();
   ScoreShared<TH>& sh = score_shared<TH>();
-  constexpr size_t kOwn = TOP ? sizeof(ScoreShared<TH>) : offsetof(ScoreShared<TH>, unit_sum);
-  SliceResult* slices = reinterpret_cast<SliceResult*>(score_smem + ((kOwn + 15) & ~size_t(15)));
+  const Units un = units_of<TH>(TOP ? p.units : 0);
+  SliceResult* slices = reinterpret_cast<SliceResult*>(
+      score_smem + units_offset<TH>() + (TOP ? ((size_t)p.units * Units::kBytes + 15) / 16 * 16 : 0));
   constexpr int N = Elem<TIn>::N;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = (int)cluster_size(), me = C > 1 ? (int)cluster_rank() : 0;
@@ -595,8 +616,8 @@ __global__ void __launch_bounds__(TH, TH == 128 ? (TOP ? 6 : 8) : 1) token_score
         unit.merge(group_sum<TIn, kUnroll>(v, gm));
       }
       if (TOP) {
-        sh.unit_key[slot * TH + tid] = key;
-        sh.unit_sum[slot * TH + tid] = unit.s;
+        un.key[slot * TH + tid] = key;
+        un.sum[slot * TH + tid] = unit.s;
       }
       acc.merge(unit);
     }
@@ -625,7 +646,7 @@ __global__ void __launch_bounds__(TH, TH == 128 ? (TOP ? 6 : 8) : 1) token_score
     Mass rest = {kLowest, 0.f};
     int n_top = 0;
     if (TOP && sound && (C > 1 || tot.s > 0.f)) {
-      n_top = select_top<TIn, TH>(s, K, tot.m, slots, p.status);
+      n_top = select_top<TIn, TH>(s, K, tot.m, slots, p.units, p.status);
       rest = sh.rest;
     }
 
@@ -875,12 +896,17 @@ __global__ void __launch_bounds__(kBwdThreads, 4) token_scores_bwd_kernel(const 
 }
 
 template <typename TIn, int TH, bool TOP>
-cudaError_t launch_scores(const ScoreParams& p, int64_t clusters, int C, cudaStream_t s) {
-  size_t smem = TOP ? sizeof(ScoreShared<TH>) : offsetof(ScoreShared<TH>, unit_sum);
-  smem = (smem + 15) & ~size_t(15);
+cudaError_t launch_scores(ScoreParams p, int64_t clusters, int C, cudaStream_t s) {
+  auto room = [](size_t units, int slices) {
+    return units_offset<TH>() + (units * Units::kBytes + 15) / 16 * 16 + slices * sizeof(SliceResult);
+  };
+  // what the longest slice needs: its pieces (the first and the last of a row may be partial) in kSlots units to a thread at most
+  const int64_t pieces = (p.V / Elem<TIn>::N + C - 1) / C, trips = (pieces + kUnroll * TH - 1) / (kUnroll * TH);
+  const int64_t groups = trips <= kSlots ? 1 : (trips + kSlots - 1) / kSlots;
+  p.units = TOP ? (int)((trips + groups - 1) / groups) * TH : 0;
+  const size_t smem = room(p.units, C > 1 ? C : 0);
   // (one limit for every launch of this kernel: launches of other threads may come in between)
-  constexpr size_t limit = sizeof(ScoreShared<TH>) + 16 + kMaxClusterX * sizeof(SliceResult);
-  if (C > 1) smem += C * sizeof(SliceResult);
+  constexpr size_t limit = units_offset<TH>() + kSlots * TH * Units::kBytes + kMaxClusterX * sizeof(SliceResult);
   const cudaError_t e = cudaFuncSetAttribute(token_scores_kernel<TIn, TH, TOP>,
                                              cudaFuncAttributeMaxDynamicSharedMemorySize, (int)limit);
   if (e != cudaSuccess) return e;
