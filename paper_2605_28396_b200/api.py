@@ -519,15 +519,25 @@ def adwin_lmhead_weight_align(hidden_student, w_student, hidden_teacher, w_teach
                            gsq=gsq, dev_status=dev_status, candidates=cands, workspace=workspace)
 
 
+def _call(device, fn, *args):
+    """A call whose kernels run on `device`, whichever device is the current one."""
+    i = device.index
+    if i is None or i == torch.cuda.current_device():
+        _check(fn(*args))
+    else:
+        with torch.cuda.device(i):
+            _check(fn(*args))
+
+
 def _int32_arg(name, t, shape, device):
     """An index or length array the kernels read: int32, contiguous, on the call's device."""
-    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or
+    if t is not None and (t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or
                           t.device != device):
         raise ValueError(f"{name}: expected a contiguous int32 tensor of shape {shape} on {device}")
 
 
 def _f32_arg(name, t, shape, device):
-    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape or
+    if t is not None and (t.dtype != torch.float32 or t.shape != shape or
                           not t.is_contiguous() or t.device != device):
         raise ValueError(f"{name}: expected a contiguous float32 tensor of shape {shape} on {device}")
 
@@ -582,10 +592,9 @@ def adwin_token_logprobs(logits, tokens, window=None, rollout_len=None, *, top_k
         o.rest = s[-1]
         o.top_ids = torch.empty((B, T, K), dtype=torch.int32, device=dev)
         o.top_logprobs = torch.empty((B, T, K), dtype=torch.float32, device=dev)
-    _check(lib().adwin_token_logprobs(
-        _ptr(logits), dt, B, T, V, ld, _ptr(tokens), _ptr(window), _ptr(rollout_len), K, int(flags),
-        _ptr(o.logprob), _ptr(o.entropy), _ptr(o.lse), _ptr(o.top_ids), _ptr(o.top_logprobs),
-        _ptr(o.rest), _ptr(dev_status), stream))
+    _call(dev, lib().adwin_token_logprobs, _ptr(logits), dt, B, T, V, ld, _ptr(tokens), _ptr(window),
+          _ptr(rollout_len), K, int(flags), _ptr(o.logprob), _ptr(o.entropy), _ptr(o.lse),
+          _ptr(o.top_ids), _ptr(o.top_logprobs), _ptr(o.rest), _ptr(dev_status), stream)
     return o
 
 
@@ -613,6 +622,8 @@ def adwin_token_logprobs_bwd(logits, tokens, lse, window=None, rollout_len=None,
     if d_top is not None:
         K = d_top.shape[-1]
         _f32_arg("d_top", d_top, (B, T, K), dev)
+        if top_ids is None:
+            raise ValueError("d_top needs top_ids")
         _int32_arg("top_ids", top_ids, (B, T, K), dev)
         if K == 0:
             d_top = None
@@ -623,10 +634,10 @@ def adwin_token_logprobs_bwd(logits, tokens, lse, window=None, rollout_len=None,
     ld_grad = _logit_rows(grad)[3]
     dt, gdt = _dtype_code(logits.dtype), _dtype_code(grad.dtype)
     dev_status, flags = _own_status(dev_status, dev, B * T, flags)
-    _check(lib().adwin_token_logprobs_bwd(
-        _ptr(logits), dt, B, T, V, ld, _ptr(tokens), _ptr(window), _ptr(rollout_len), _ptr(lse),
-        _ptr(entropy), _ptr(d_logprob), _ptr(d_entropy), _ptr(top_ids), _ptr(d_top), K, int(flags),
-        _ptr(grad), gdt, ld_grad, _ptr(dev_status), stream))
+    _call(dev, lib().adwin_token_logprobs_bwd, _ptr(logits), dt, B, T, V, ld, _ptr(tokens),
+          _ptr(window), _ptr(rollout_len), _ptr(lse), _ptr(entropy), _ptr(d_logprob),
+          _ptr(d_entropy), _ptr(top_ids), _ptr(d_top), K, int(flags), _ptr(grad), gdt, ld_grad,
+          _ptr(dev_status), stream)
     return SimpleNamespace(grad=grad, dev_status=dev_status)
 
 
@@ -663,11 +674,10 @@ def adwin_opd_topk_kl_fwd_bwd(student, tokens, top_ids, top_logprobs, window, ro
     s = _scalars(2 + (1 if want_gsq else 0) + (1 if want_lse else 0), B, T, dev)
     o = SimpleNamespace(kl=s[0], logratio=s[1], gsq=s[2] if want_gsq else None,
                         lse_s=s[-1] if want_lse else None, grad=grad, dev_status=dev_status)
-    _check(lib().adwin_opd_topk_kl_fwd_bwd(
-        _ptr(student), dt, B, T, V, ld, _ptr(tokens), _ptr(window), _ptr(rollout_len), _ptr(top_ids),
-        _ptr(top_logprobs), _ptr(rest), K, float(grad_scale), int(kl_mode), int(flags), _ptr(grad),
-        gdt, ld_grad, _ptr(o.kl), _ptr(o.logratio), _ptr(o.gsq), _ptr(o.lse_s), _ptr(dev_status),
-        stream))
+    _call(dev, lib().adwin_opd_topk_kl_fwd_bwd, _ptr(student), dt, B, T, V, ld, _ptr(tokens),
+          _ptr(window), _ptr(rollout_len), _ptr(top_ids), _ptr(top_logprobs), _ptr(rest), K,
+          float(grad_scale), int(kl_mode), int(flags), _ptr(grad), gdt, ld_grad, _ptr(o.kl),
+          _ptr(o.logratio), _ptr(o.gsq), _ptr(o.lse_s), _ptr(dev_status), stream)
     return o
 
 
@@ -701,8 +711,8 @@ def adwin_quantize_rows_i8(x, *, flags=0, dev_status=None):
     ldq = -(-d // 16) * 16
     q = torch.empty((*x.shape[:-1], ldq), dtype=torch.int8, device=dev)
     scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
-    _check(lib().adwin_quantize_rows_i8(_ptr(x), dt, M, d, ld, _ptr(q), ldq, _ptr(scale), int(flags),
-                                        _ptr(dev_status), stream))
+    _call(dev, lib().adwin_quantize_rows_i8, _ptr(x), dt, M, d, ld, _ptr(q), ldq, _ptr(scale),
+          int(flags), _ptr(dev_status), stream)
     return (q if ldq == d else q[..., :d]), scale
 
 
@@ -729,6 +739,6 @@ def adwin_linear_i8(x, x_scale, w, w_scale, *, out=None, out_dtype=torch.bfloat1
     ldx, ldw = (-(-d // 16) * 16 if n <= 1 else ld for n, ld in ((M, ldx), (N, ldw)))
     odt = _dtype_code(out.dtype)
     dev_status, flags = _own_status(dev_status, dev, M, flags)
-    _check(lib().adwin_linear_i8(_ptr(x), ldx, _ptr(x_scale), _ptr(w), ldw, _ptr(w_scale), M, N, d,
-                                 _ptr(out), odt, ldo, int(flags), _ptr(dev_status), stream))
+    _call(dev, lib().adwin_linear_i8, _ptr(x), ldx, _ptr(x_scale), _ptr(w), ldw, _ptr(w_scale), M, N,
+          d, _ptr(out), odt, ldo, int(flags), _ptr(dev_status), stream)
     return out
