@@ -523,10 +523,12 @@ def _call(device, fn, *args):
     """A call whose kernels run on `device`, whichever device is the current one."""
     i = device.index
     if i is None or i == torch.cuda.current_device():
-        _check(fn(*args))
+        rc = fn(*args)
     else:
         with torch.cuda.device(i):
-            _check(fn(*args))
+            rc = fn(*args)
+    if rc != OK:
+        raise AdwinError(rc)
 
 
 def _int32_arg(name, t, shape, device):
@@ -583,15 +585,15 @@ def adwin_token_logprobs(logits, tokens, window=None, rollout_len=None, *, top_k
         raise ValueError(f"top_k must be between 0 and min(V, {TOP_MAX})")
     dt = _dtype_code(logits.dtype)
     dev_status, flags = _own_status(dev_status, dev, B * T, flags)
-    # one allocation for the scalars, one for the alternatives' scores
     s = _scalars(1 + (1 if want_entropy else 0) + (1 if want_lse else 0) + (1 if K else 0), B, T, dev)
-    o = SimpleNamespace(logprob=s[0], entropy=s[1] if want_entropy else None,
-                        lse=s[2 if want_entropy else 1] if want_lse else None, top_ids=None,
-                        top_logprobs=None, rest=None, dev_status=dev_status)
+    rest = ids = top = None
     if K:
-        o.rest = s[-1]
-        o.top_ids = torch.empty((B, T, K), dtype=torch.int32, device=dev)
-        o.top_logprobs = torch.empty((B, T, K), dtype=torch.float32, device=dev)
+        rest = s[-1]
+        top = torch.empty((B, T, K), dtype=torch.float32, device=dev)
+        ids = torch.empty((B, T, K), dtype=torch.int32, device=dev)
+    o = SimpleNamespace(logprob=s[0], entropy=s[1] if want_entropy else None,
+                        lse=s[2 if want_entropy else 1] if want_lse else None, top_ids=ids,
+                        top_logprobs=top, rest=rest, dev_status=dev_status)
     _call(dev, lib().adwin_token_logprobs, _ptr(logits), dt, B, T, V, ld, _ptr(tokens), _ptr(window),
           _ptr(rollout_len), K, int(flags), _ptr(o.logprob), _ptr(o.entropy), _ptr(o.lse),
           _ptr(o.top_ids), _ptr(o.top_logprobs), _ptr(o.rest), _ptr(dev_status), stream)

@@ -1,6 +1,8 @@
 // Host-side declarations shared by the translation units of the library (not installed).
 #pragma once
 
+#include <atomic>
+
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -31,6 +33,21 @@ cudaError_t launch_chained(void (*kernel)(P...), unsigned grid, int threads, siz
   cfg.attrs = attr;
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// Sets a kernel's dynamic shared memory limit, the first time on every device (2 us of a small call).  `Kernel`
+// keeps one limit for all its launches.
+template <auto Kernel>
+cudaError_t shared_limit(size_t bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (bit && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 struct KlParams;

@@ -413,8 +413,7 @@ template <typename TOut, int NT>
 cudaError_t launch_few(const FewParams& p, int sm_count, cudaStream_t s) {
   const size_t smem = (size_t)NT * 8 * p.pitch + (size_t)kFewGroups * 2 * 3 * NT * 4 * 32 * 4;
   constexpr size_t limit = kFewSmemX + (size_t)kFewGroups * 2 * 3 * NT * 4 * 32 * 4;
-  const cudaError_t e = cudaFuncSetAttribute(linear_i8_few_kernel<TOut, NT>,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)limit);
+  const cudaError_t e = shared_limit<linear_i8_few_kernel<TOut, NT>>(limit);
   if (e != cudaSuccess) return e;
   int64_t grid = (int64_t)sm_count * kFewCtas, tiles = ((p.N + 15) / 16 + kFewGroups - 1) / kFewGroups;
   if (grid > tiles) grid = tiles;
@@ -461,12 +460,12 @@ cudaError_t launch_linear_i8(const int8_t* x, int64_t ldx, const float* step_x, 
   p.limit_ns = handshake_wait_limit_ns();
   CUtensorMap mx, mw;
   if (!make_map_i8(&mx, x, d, M, ldx, kBM) || !make_map_i8(&mw, w, d, N, ldw, kBM)) return cudaErrorInvalidValue;
-  auto launch = [&](auto kernel) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
-    if (e != cudaSuccess) return e;
-    return launch_chained(kernel, (unsigned)(sm_count & ~1), kThreads, kLinearSmem, 2, s, mx, mw, p);
-  };
-  return out_dtype == ADWIN_BF16 ? launch(linear_i8_kernel<__nv_bfloat16>) : launch(linear_i8_kernel<float>);
+  const bool bf = out_dtype == ADWIN_BF16;
+  const cudaError_t e = bf ? shared_limit<linear_i8_kernel<__nv_bfloat16>>(kLinearSmem)
+                           : shared_limit<linear_i8_kernel<float>>(kLinearSmem);
+  if (e != cudaSuccess) return e;
+  return launch_chained(bf ? linear_i8_kernel<__nv_bfloat16> : linear_i8_kernel<float>, (unsigned)(sm_count & ~1),
+                        kThreads, kLinearSmem, 2, s, mx, mw, p);
 }
 
 }  // namespace adwin

@@ -907,8 +907,7 @@ cudaError_t launch_scores(ScoreParams p, int64_t clusters, int C, cudaStream_t s
   const size_t smem = room(p.units, C > 1 ? C : 0);
   // (one limit for every launch of this kernel: launches of other threads may come in between)
   constexpr size_t limit = units_offset<TH>() + kSlots * TH * Units::kBytes + kMaxClusterX * sizeof(SliceResult);
-  const cudaError_t e = cudaFuncSetAttribute(token_scores_kernel<TIn, TH, TOP>,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, (int)limit);
+  const cudaError_t e = shared_limit<token_scores_kernel<TIn, TH, TOP>>(limit);
   if (e != cudaSuccess) return e;
   return launch_chained(token_scores_kernel<TIn, TH, TOP>, (unsigned)(clusters * C), TH, smem, C, s, p);
 }

@@ -718,7 +718,7 @@ template <typename TIn, typename TOut, int TH, int CTAS>
 cudaError_t launch_plan(const TopkParams& p, int C, int64_t rows, int sm_count, cudaStream_t s) {
   const size_t smem = sizeof(TopkShared<TH>);
   auto kernel = topk_kl_kernel<TIn, TOut, TH, CTAS>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t e = shared_limit<topk_kl_kernel<TIn, TOut, TH, CTAS>>(smem);
   if (e != cudaSuccess) return e;
   // as many clusters as the GPU holds at a time: their CTAs go on from row to row
   static std::atomic<int> held[4];
