@@ -10,9 +10,9 @@
 // in tensor memory (exact: d < 2^17 keeps every sum below 2^31), operands by TMA in the 128-byte
 // swizzle, 128 entries of the contraction a k-block.  The pipeline is that of tc_pipeline.cuh: bytes
 // are laid out as for 64 bf16.  An accumulator becomes float(acc) * (step_x * step_w): three roundings.
-// 4 096 x 2 560 against 151 936 channels: 1.23 ms (2.58 PFLOP/s; the tensor pipe is busy 72 % of the time, then the
-// power limit).  Rows of out that start off 16-byte boundaries leave through shared memory, a row of 32 results at a
-// time (777 x 1 000 against 50 257 channels, fp32 out: 294 us with scattered 4-byte stores, 114 so).
+// The results leave through shared memory as whole pieces of rows: 4 096 x 2 560 against 151 936 channels 1.11 to 1.18 ms
+// (2.7 to 2.9 POP/s, then the power limit) where 16-byte stores of a lane's own row took 1.19 to 1.23; 777 x 1 000
+// against 50 257 channels (rows off 16-byte boundaries, fp32) 81 us, 294 with scattered 4-byte stores, 114 in pieces of 32.
 #include <cuda_bf16.h>
 
 #include "adwin_common.cuh"
@@ -120,11 +120,14 @@ struct LinearParams {
   int32_t* status;
   uint64_t limit_ns;
 };
-// Behind the stages: 32 x 32 results per epilogue warp on their way into rows of out that start anywhere.
-constexpr int kTurnPitch = 33;
-constexpr int kTurnBytes = 32 * kTurnPitch * 4;
-constexpr int kLinearSmem = kSmemBytes + (kEpiThreads / 32) * kTurnBytes;
-static_assert(kLinearSmem <= 227 * 1024, "shared memory");
+// Behind the stages: per epilogue warp 32 rows of 64 results on their way out (16-byte units XOR-swizzled with
+// the row).
+constexpr int kStages = 5;
+template <typename TOut>
+__host__ __device__ constexpr int out_row() { return 64 * (int)sizeof(TOut); }   // bytes: 64 results
+constexpr int kWarpBytes = 32 * out_row<float>();
+constexpr int kLinearSmem = kCtrlBytes + 1024 + kStages * kPairStageBytes + (kEpiThreads / 32) * kWarpBytes;
+static_assert(kLinearSmem <= 227 * 1024 && kStages <= kPairStages, "shared memory");
 
 // Tile t: groups of kGroupM row tiles, within one the row tiles of a column tile follow one another, so
 // that W passes through once a group and the group's rows of x stay in L2.
@@ -171,7 +174,7 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
         tile_of(p, t, pm, n);
         const int m0 = (2 * pm + (int)rank) * kBM, n0 = n * kBN + (int)rank * (kBN / 2);
         for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-          const uint32_t s = it % kPairStages, ph = (it / kPairStages) & 1;
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1;
           if (!bar_wait(smem_addr(&ctrl->empty[s]), ph ^ 1, abort, p.limit_ns)) { ok = false; break; }
           const uint32_t bar = smem_addr(&ctrl->full[s]);
           const uint32_t a = stage0 + s * kPairStageBytes, b = a + kABytes;
@@ -181,7 +184,11 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
           tma_load_2d_pair(b, &map_w, kb * kBKBytes, n0, bar0);
         }
       }
-      if (!ok && rank == 0) pair_drain_loads(ctrl, it);
+      if (!ok && rank == 0) {   // give up: let the copies in flight land
+        const uint32_t n_out = it < (uint32_t)kStages ? it : (uint32_t)kStages;
+        for (uint32_t j = it - n_out; j < it; ++j)
+          bar_wait_drain(smem_addr(&ctrl->full[j % kStages]), (j / kStages) & 1);
+      }
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
@@ -193,7 +200,7 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
         tc_fence_after_sync();
         const uint32_t tmem_d = tmem_base + slot * kBN;
         for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-          const uint32_t s = it % kPairStages, ph = (it / kPairStages) & 1;
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1;
           if (!bar_wait(smem_addr(&ctrl->full[s]), ph, abort, p.limit_ns)) { ok = false; break; }
           tc_fence_after_sync();
           const uint32_t a = stage0 + s * kPairStageBytes, b = a + kABytes;
@@ -212,65 +219,71 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       }
     }
   } else if (warp >= kEpiWarp0) {
+    // A lane holds a row of the accumulator.  Its results go through shared memory, so that they leave
+    // as whole pieces of rows: 16 bytes a lane along a row where rows start on 16-byte boundaries, an
+    // entry a lane otherwise.
     const int quad = warp & 3, half = (warp - kEpiWarp0) >> 2;
-    const int row = quad * 32 + lane;
+    uint8_t* const mine = smem_raw + (stage0 - smem_addr(smem_raw)) + kStages * kPairStageBytes + (warp - kEpiWarp0) * kWarpBytes;
+    constexpr int kOutRow = out_row<TOut>(), kUnits = kOutRow / 16, kPass = 64;   // columns that go out at a time
     uint32_t acc_it = 0;
     for (int64_t t = pair; t < tiles; t += pairs, ++acc_it) {
       int pm, nt;
       tile_of(p, t, pm, nt);
       const uint32_t slot = acc_it & 1, aph = (acc_it >> 1) & 1;
-      const int64_t m = (int64_t)(2 * pm + (int)rank) * kBM + row;
-      const int64_t n0 = (int64_t)nt * kBN + half * 128;
-      const float sx = m < p.M ? p.step_x[m] : 0.f;
-      TOut* o = static_cast<TOut*>(p.out) + (m < p.M ? m : 0) * p.ldo + n0;
+      const int64_t m0 = (int64_t)(2 * pm + (int)rank) * kBM + quad * 32, n0 = (int64_t)nt * kBN + half * 128;
+      const int rows = p.M - m0 < 32 ? (p.M > m0 ? (int)(p.M - m0) : 0) : 32;
+      const int cols = p.N - n0 < 128 ? (p.N > n0 ? (int)(p.N - n0) : 0) : 128;
+      const float sx = lane < rows ? __ldg(p.step_x + m0 + lane) : 0.f;
       if (!__all_sync(0xffffffffu, bar_wait(smem_addr(&ctrl->acc_full[slot]), aph, abort, p.limit_ns))) break;
       tc_fence_after_sync();
       const uint32_t t_lane = tmem_base + ((uint32_t)(quad * 32) << 16) + slot * kBN + (uint32_t)(half * 128);
-      float* turn = reinterpret_cast<float*>(smem_raw + (stage0 - smem_addr(smem_raw)) + kPairStages * kPairStageBytes) +
-                    (warp - kEpiWarp0) * (kTurnBytes / 4);
+      const int passes = rows > 0 ? (cols + kPass - 1) / kPass : 0;
 #pragma unroll 1
-      for (int j = 0; j < 4; ++j) {
-        const int64_t nj = n0 + j * 32;
-        const int left = nj >= p.N ? 0 : (p.N - nj < 32 ? (int)(p.N - nj) : 32);
-        if (left == 0) break;
-        uint32_t r[32];
-        __syncwarp();   // (the load is the warp's)
-        tmem_ld32(t_lane + j * 32, r);
-        tmem_ld_wait();
-        TOut* oj = o + j * 32;
-        if (p.whole && left == 32) {
-          if (m < p.M) {
-            float v[32];
+      for (int pass = 0; pass < passes; ++pass) {
+        __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = (float)(int)r[i] * (sx * __ldg(p.step_w + nj + i));
-            if (sizeof(TOut) == 2) {
+        for (int j = 0; j < kPass / 32; ++j) {
+          uint32_t r[32];
+          tmem_ld32(t_lane + pass * kPass + j * 32, r);
+          tmem_ld_wait();
+          const int c0 = pass * kPass + j * 32;
+          const float sw = c0 + lane < cols ? __ldg(p.step_w + n0 + c0 + lane) : 0.f;   // column c0 + lane's
+          constexpr int kUnit = 16 / (int)sizeof(TOut);   // results of a 16-byte unit
 #pragma unroll
-              for (int i = 0; i < 32; i += 8)
-                *reinterpret_cast<uint4*>(oj + i) =
-                    make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
-                               pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
-            } else {
+          for (int u = 0; u < 32 / kUnit; ++u) {
+            float v[kUnit];
 #pragma unroll
-              for (int i = 0; i < 32; i += 4)
-                *reinterpret_cast<float4*>(oj + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-            }
+            for (int i = 0; i < kUnit; ++i)
+              v[i] = (float)(int)r[u * kUnit + i] * (sx * __shfl_sync(0xffffffffu, sw, u * kUnit + i));
+            uint4 x;
+            if (sizeof(TOut) == 2)
+              x = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4 % kUnit], v[5 % kUnit]),
+                             pack_bf16x2(v[6 % kUnit], v[7 % kUnit]));
+            else
+              x = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+            const int unit = j * (32 / kUnit) + u;
+            *reinterpret_cast<uint4*>(mine + lane * kOutRow + ((unit ^ (lane & (kUnits - 1))) << 4)) = x;
+          }
+        }
+        __syncwarp();
+        const int left = cols - pass * kPass < kPass ? cols - pass * kPass : kPass;
+        TOut* o = static_cast<TOut*>(p.out) + m0 * p.ldo + n0 + pass * kPass;
+        if (p.whole && left == kPass) {
+          const int unit = lane % kUnits;
+          for (int i = lane / kUnits; i < rows; i += 32 / kUnits) {
+            const uint4 x = *reinterpret_cast<const uint4*>(mine + i * kOutRow + ((unit ^ (i & (kUnits - 1))) << 4));
+            __stcs(reinterpret_cast<uint4*>(o + i * p.ldo) + unit, x);
           }
         } else {
-          // a lane holds a row's 32 results; turned over in shared memory it holds a column's, and a row goes out
-          // in one piece wherever it starts
-#pragma unroll
-          for (int i = 0; i < 32; ++i) turn[lane * kTurnPitch + i] = (float)(int)r[i];
-          __syncwarp();
-          const int64_t m0 = m - lane;
-          const int rows = p.M - m0 < 32 ? (p.M > m0 ? (int)(p.M - m0) : 0) : 32;
-          const float sw = lane < left ? __ldg(p.step_w + nj + lane) : 0.f;
-          TOut* col = static_cast<TOut*>(p.out) + m0 * p.ldo + nj + lane;
-#pragma unroll 8
           for (int i = 0; i < rows; ++i) {
-            const float s = __shfl_sync(0xffffffffu, sx, i);
-            if (lane < left) Elem<TOut>::store1(col + i * p.ldo, 0, turn[i * kTurnPitch + lane] * (s * sw));
+            const TOut* row = reinterpret_cast<const TOut*>(mine + i * kOutRow);
+            constexpr int kUnit = 16 / (int)sizeof(TOut);
+#pragma unroll
+            for (int k = 0; k < kPass / 32; ++k) {
+              const int c = k * 32 + lane;
+              if (c < left) o[i * p.ldo + c] = row[((c / kUnit) ^ (i & (kUnits - 1))) * kUnit + c % kUnit];
+            }
           }
-          __syncwarp();
         }
       }
       tc_fence_before_sync();
