@@ -594,6 +594,12 @@ struct TopkCta {
       for (int j = tid, slot = 0; j < np; j += kGroup * TH, slot += kGroup) {
         uint4 v[kGroup];
         take(j, first, v);
+        // the next group's lines on their way into L2 (5 120 rows of 151 936 bf16 entries: 720 -> 690 us)
+        if ((lane & 7) == 0) {
+#pragma unroll
+          for (int k = 0; k < kGroup; ++k)
+            if (j + (k + kGroup) * TH < np) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + j + (k + kGroup) * TH));
+        }
         if (marked >> (slot & 31) & ((1u << kGroup) - 1)) {
           for (int x = l.first[tid & (kChains - 1)]; x >= 0; x = l.next[x]) {
             if (l.owner[x] != tid) continue;
@@ -643,19 +649,6 @@ struct TopkCta {
           Pairs<TIn>::make(v[k], z);
 #pragma unroll
           for (int x = 0; x < NP; ++x) g[x] = mul2(coef, ex2_2(mul2(add2(z[x], neg_m), splat2(kLog2e))));
-          if (any) {
-            for (int y = l.first[tid & (kChains - 1)]; y >= 0; y = l.next[y]) {
-              if (l.owner[y] != tid || l.slot[y] != slot + k || !l.counts[y]) continue;
-              const int e = (l.id[y] - entry0) & (N - 1);
-              const float gl = p.alpha * listed_grad(sh.scalars, l.z[y], l.lq[y], p.forward);
-#pragma unroll
-              for (int x = 0; x < NP; ++x) {
-                float a, b;
-                upk2(g[x], a, b);
-                g[x] = pk2(e == 2 * x ? gl : a, e == 2 * x + 1 ? gl : b);
-              }
-            }
-          }
           char* o = out + (size_t)(j + k * TH) * kOutPiece;
           if (wide) {
             store_pairs<TOut>(o, g);
@@ -667,6 +660,14 @@ struct TopkCta {
               Elem<TOut>::store1(o, 2 * x, a);
               Elem<TOut>::store1(o, 2 * x + 1, b);
             }
+          }
+        }
+        if (any) {   // the listed entries among them once more (a thread's stores to one place keep their order)
+#pragma unroll 1
+          for (int x = l.first[tid & (kChains - 1)]; x >= 0; x = l.next[x]) {
+            if (l.owner[x] != tid || l.slot[x] < slot || l.slot[x] >= slot + kGroup || !l.counts[x]) continue;
+            const float gl = p.alpha * listed_grad(sh.scalars, l.z[x], l.lq[x], p.forward);
+            Elem<TOut>::store1(out, l.id[x] - entry0, gl);
           }
         }
       }
