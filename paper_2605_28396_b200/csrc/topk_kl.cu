@@ -143,19 +143,19 @@ __device__ __forceinline__ uint4 masked_piece() {
   constexpr uint32_t w = sizeof(TIn) == 2 ? 0xff80ff80u : 0xff800000u;   // -infinity
   return make_uint4(w, w, w, w);
 }
-template <typename TIn>
-__device__ __forceinline__ void mask_entry(uint4& v, int e) {
-  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// Entry `e` of a group of pieces becomes -infinity.
+template <typename TIn, int U>
+__device__ __forceinline__ void mask_entry(uint4 (&v)[U], int e) {
+  const int word = sizeof(TIn) == 4 ? e : e >> 1;
+  const uint32_t keep = sizeof(TIn) == 4 ? 0u : (e & 1 ? 0xffffu : 0xffff0000u);
+  const uint32_t put = sizeof(TIn) == 4 || (e & 1) ? 0xff800000u : 0xff80u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (sizeof(TIn) == 4) {
-      if (e == i) w[i] = 0xff800000u;
-    } else {
-      if (e == 2 * i) w[i] = (w[i] & 0xffff0000u) | 0xff80u;
-      if (e == 2 * i + 1) w[i] = (w[i] & 0xffffu) | 0xff800000u;
-    }
+  for (int k = 0; k < U; ++k) {
+    if (word == 4 * k) v[k].x = (v[k].x & keep) | put;
+    if (word == 4 * k + 1) v[k].y = (v[k].y & keep) | put;
+    if (word == 4 * k + 2) v[k].z = (v[k].z & keep) | put;
+    if (word == 4 * k + 3) v[k].w = (v[k].w & keep) | put;
   }
-  v = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Sums over entries of the rest, of one thread.
@@ -601,12 +601,10 @@ struct TopkCta {
             if (j + (k + kGroup) * TH < np) asm volatile("prefetch.global.L2 [%0];" ::"l"(src + j + (k + kGroup) * TH));
         }
         if (marked >> (slot & 31) & ((1u << kGroup) - 1)) {
+#pragma unroll 1
           for (int x = l.first[tid & (kChains - 1)]; x >= 0; x = l.next[x]) {
-            if (l.owner[x] != tid) continue;
-            const int at = l.slot[x] - slot, e = (l.id[x] - entry0) & (N - 1);
-#pragma unroll
-            for (int k = 0; k < kGroup; ++k)
-              if (at == k) mask_entry<TIn>(v[k], e);
+            const int at = l.slot[x] - slot;
+            if (l.owner[x] == tid && at >= 0 && at < kGroup) mask_entry<TIn>(v, at * N + ((l.id[x] - entry0) & (N - 1)));
           }
         }
         acc.raise(group_max(v, static_cast<TIn*>(nullptr)));
@@ -637,29 +635,38 @@ struct TopkCta {
       constexpr int kOutPiece = N * (int)sizeof(TOut), kOutAlign = kOutPiece < 16 ? kOutPiece : 16;
       const bool wide = (reinterpret_cast<uintptr_t>(out) & (kOutAlign - 1)) == 0;
       const f2_t neg_m = splat2(-sh.scalars.m_rest), coef = splat2(p.alpha * sh.scalars.c_rest);
+      auto gradient = [&](const uint4& v, f2_t (&g)[NP]) {
+        f2_t z[NP];
+        Pairs<TIn>::make(v, z);
+#pragma unroll
+        for (int x = 0; x < NP; ++x) g[x] = mul2(coef, ex2_2(mul2(add2(z[x], neg_m), splat2(kLog2e))));
+      };
+      if (!wide) {   // rows of the gradient off its pieces' boundaries: an entry at a time
+#pragma unroll 1
+        for (int j = tid; j < np; j += TH) {
+          f2_t g[NP];
+          gradient(read16(src + j, drop), g);
+#pragma unroll
+          for (int x = 0; x < NP; ++x) {
+            float a, b;
+            upk2(g[x], a, b);
+            Elem<TOut>::store1(out, (int64_t)j * N + 2 * x, a);
+            Elem<TOut>::store1(out, (int64_t)j * N + 2 * x + 1, b);
+          }
+        }
+      }
 #pragma unroll 1
       for (int j = tid, slot = 0; j < np; j += kGroup * TH, slot += kGroup) {
-        uint4 v[kGroup];
-        take(j, drop, v);
         const bool any = marked >> (slot & 31) & ((1u << kGroup) - 1);
+        if (wide) {
+          uint4 v[kGroup];
+          take(j, drop, v);
 #pragma unroll
-        for (int k = 0; k < kGroup; ++k) {
-          if (j + k * TH >= np) break;
-          f2_t z[NP], g[NP];
-          Pairs<TIn>::make(v[k], z);
-#pragma unroll
-          for (int x = 0; x < NP; ++x) g[x] = mul2(coef, ex2_2(mul2(add2(z[x], neg_m), splat2(kLog2e))));
-          char* o = out + (size_t)(j + k * TH) * kOutPiece;
-          if (wide) {
-            store_pairs<TOut>(o, g);
-          } else {
-#pragma unroll
-            for (int x = 0; x < NP; ++x) {
-              float a, b;
-              upk2(g[x], a, b);
-              Elem<TOut>::store1(o, 2 * x, a);
-              Elem<TOut>::store1(o, 2 * x + 1, b);
-            }
+          for (int k = 0; k < kGroup; ++k) {
+            if (j + k * TH >= np) break;
+            f2_t g[NP];
+            gradient(v[k], g);
+            store_pairs<TOut>(out + (size_t)(j + k * TH) * kOutPiece, g);
           }
         }
         if (any) {   // the listed entries among them once more (a thread's stores to one place keep their order)
