@@ -759,16 +759,16 @@ cudaError_t launch(const TopkParams& p, int64_t rows, int sm_count, cudaStream_t
   // few rows: several CTAs to a row, as long as each has two groups of pieces to a thread
   int C = 1;
   while (C < kMaxCtas && rows * C * 2 <= sm_count && pieces >= (int64_t)C * 2 * 1024) C *= 2;
-  // Many: as many threads to a row as leave its shorter half a group of pieces each, 32 warps per SM in all; and not
-  // many more than 45 MB of rows at a time, or their second read misses L2 (bf16, us for 128 threads x 8
-  // CTAs per SM / 256 x 4 / 512 x 2 / 512 x 2 in pairs: 18 432 rows of 4 096 entries 284 / 369 / 552 / -,
-  // 2 560 of 32 000 161 / 155 / 164 / 208, 2 300 of 50 257 131 / 118 / 121 / 149, 5 120 of 151 936
-  // - / - / 735 / 720).
+  // Many: as many threads to a row as leave each a few groups of pieces, about 32 warps per SM in all (bf16, us for 128
+  // threads x 8 CTAs per SM / 256 x 4 / 512 x 2 / 960 x 1: 18 432 rows of 4 096 entries 225 / 369 / 552 / -,
+  // 2 560 of 32 000 139 / 129 / 136 / -, 2 300 of 50 257 116 / 104 / 107 / -, 5 120 of 151 936 - / - / 652 / 609;
+  // the last with 512 x 2 in pairs 630, 256 x 4 in pairs 678)
   const bool few = rows * C <= sm_count;
   if (pieces / C < (few ? 1024 : 3000)) return launch_plan<TIn, TOut, 128, 8>(p, C, rows, sm_count, s);
-  if (pieces / C < (few ? 4096 : 8192)) return launch_plan<TIn, TOut, 256, 4>(p, C, rows, sm_count, s);
-  if (C == 1) C = 2;
-  return launch_plan<TIn, TOut, 512, 2>(p, C, rows, sm_count, s);
+  if (pieces / C < (few ? 4096 : 10000)) return launch_plan<TIn, TOut, 256, 4>(p, C, rows, sm_count, s);
+  // and not many more than 45 MB of rows at a time, or their second read misses L2
+  while (C < kMaxCtas && sm_count / C * p.V * (int64_t)sizeof(TIn) > (int64_t(50) << 20)) C *= 2;
+  return launch_plan<TIn, TOut, 960, 1>(p, C, rows, sm_count, s);
 }
 
 }  // namespace
