@@ -114,7 +114,7 @@ struct ScoreParams {
   int64_t V, ld;
   RowRange range;
   const int32_t* tokens;
-  int K, units;                     // units: room for those of a CTA's slice
+  int K, units, groups;             // units: room for those of a CTA's slice; groups: of loads per unit
   float *logprob, *entropy, *lse;   // entropy, lse: may be null
   int32_t* top_ids;
   float *top_logprobs, *rest;       // rest: may be null
@@ -576,7 +576,7 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
     if (me == C - 1 && tid >= 32 && tid - 32 < rp.tail) s.edge = (int)p.V - rp.tail + (tid - 32);
     s.edge_z = s.edge >= 0 ? Elem<TIn>::load1(s.row, s.edge) : 0.f;
     const int trips = (s.np + kUnroll * TH - 1) / (kUnroll * TH);
-    s.groups = trips <= kSlots ? 1 : (trips + kSlots - 1) / kSlots;
+    s.groups = p.groups;   // (of the longest slice: a row with a piece less must not take more room than that)
     const int slots = s.groups == 1 ? trips : (trips + s.groups - 1) / s.groups;
     const int y = (me == 0 && tid == 0) ? p.tokens[r] : 0;
     const bool y_valid = y >= 0 && (int64_t)y < p.V;
@@ -615,7 +615,7 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
         if (TOP && i < s.np) key = max(key, order_key(gm));
         unit.merge(group_sum<TIn, kUnroll>(v, gm));
       }
-      if (TOP) {
+      if (TOP && ADWIN_CHK(slot * TH + tid < p.units, p.status)) {
         un.key[slot * TH + tid] = key;
         un.sum[slot * TH + tid] = unit.s;
       }
@@ -904,6 +904,7 @@ cudaError_t launch_scores(ScoreParams p, int64_t clusters, int C, cudaStream_t s
   const int64_t pieces = (p.V / Elem<TIn>::N + C - 1) / C, trips = (pieces + kUnroll * TH - 1) / (kUnroll * TH);
   const int64_t groups = trips <= kSlots ? 1 : (trips + kSlots - 1) / kSlots;
   p.units = TOP ? (int)((trips + groups - 1) / groups) * TH : 0;
+  p.groups = (int)groups;
   const size_t smem = room(p.units, C > 1 ? C : 0);
   // (one limit for every launch of this kernel: launches of other threads may come in between)
   constexpr size_t limit = units_offset<TH>() + kSlots * TH * Units::kBytes + kMaxClusterX * sizeof(SliceResult);

@@ -92,6 +92,15 @@ def test_scores_at_padded_and_odd_strides(V, ld, dtype):
     _check(z, y, 10, _lengths(1, 80))
 
 
+@pytest.mark.parametrize("V,dtype", [(98313, "bf16"), (98307, "bf16"), (49159, "f32"), (8201, "bf16"), (196625, "bf16")])
+def test_scores_where_rows_differ_by_a_round_of_loads(V, dtype):
+    """Packed rows of which some have one 16-byte piece more than the others, and with it one more round of loads
+    (12 rounds of 1024 pieces are the most that a thread keeps apart)."""
+    z, y = _logits(2, 60, V, DTYPES[dtype], V)
+    for K in (1, 30):
+        _check(z, y, K)
+
+
 @pytest.mark.parametrize("many", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_scores_of_rows_whose_alternatives_are_hard_to_find(dtype, many):
