@@ -757,11 +757,10 @@ struct ScoreBwdParams {
   int32_t* status;
 };
 
-constexpr int kBwdThreads = 256;
 constexpr int kBwdUnroll = 4;
 
-template <typename TIn, typename TOut>
-__global__ void __launch_bounds__(kBwdThreads, 4) token_scores_bwd_kernel(const ScoreBwdParams p) {
+template <typename TIn, typename TOut, int TH>
+__global__ void __launch_bounds__(TH, 1024 / TH) token_scores_bwd_kernel(const ScoreBwdParams p) {
   chain();
   __shared__ RowList list;
   __shared__ int32_t own_id[ADWIN_TOP_MAX + 1];
@@ -788,12 +787,12 @@ __global__ void __launch_bounds__(kBwdThreads, 4) token_scores_bwd_kernel(const 
     const int64_t begin = part == 0 ? 0 : entry0, end = last ? p.V : entry0 + np * N;
 
     // weights of single entries: the alternatives', the token's behind them
-    if (tid <= p.K) {
+    for (int j = tid; j <= p.K; j += TH) {
       int32_t id = -1;
       float w = 0.f;
-      if (tid < p.K) {
-        id = p.top_ids[r * p.K + tid];
-        w = p.d_top[r * p.K + tid];
+      if (j < p.K) {
+        id = p.top_ids[r * p.K + j];
+        w = p.d_top[r * p.K + j];
       } else if (p.d_logprob) {
         id = p.tokens[r];
         w = p.d_logprob[r];
@@ -804,8 +803,8 @@ __global__ void __launch_bounds__(kBwdThreads, 4) token_scores_bwd_kernel(const 
         id = -1;
         w = 0.f;
       }
-      own_id[tid] = id;
-      own_w[tid] = w;
+      own_id[j] = id;
+      own_w[j] = w;
     }
     __syncthreads();
     const float h = p.d_entropy ? p.d_entropy[r] : 0.f;
@@ -823,10 +822,16 @@ __global__ void __launch_bounds__(kBwdThreads, 4) token_scores_bwd_kernel(const 
         any = some;
       }
     }
-    // this thread's single entry, read before the gradient may overwrite it (grad may be the logits)
-    const int64_t mine = tid <= p.K ? own_id[tid] : -1;
-    const bool patch = mine >= begin && mine < end;   // (none: -1)
-    const float z_mine = patch ? Elem<TIn>::load1(row, mine) : 0.f;
+    // this thread's single entries, read before the gradient may overwrite them (grad may be the logits)
+    constexpr int kMine = (ADWIN_TOP_MAX + TH) / TH;
+    int64_t mine[kMine];
+    float z_mine[kMine];
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      mine[k] = tid + k * TH <= p.K ? own_id[tid + k * TH] : -1;
+      if (mine[k] < begin || mine[k] >= end) mine[k] = -1;
+      z_mine[k] = mine[k] >= 0 ? Elem<TIn>::load1(row, mine[k]) : 0.f;
+    }
     const int64_t edge = (part == 0 && tid < rp.head) ? tid
                          : (last && tid >= 32 && tid - 32 < rp.tail) ? p.V - rp.tail + (tid - 32) : -1;
     const float z_edge = edge >= 0 ? Elem<TIn>::load1(row, edge) : 0.f;
@@ -846,16 +851,16 @@ __global__ void __launch_bounds__(kBwdThreads, 4) token_scores_bwd_kernel(const 
     constexpr int kOutAlign = N * sizeof(TOut) < 16 ? (int)(N * sizeof(TOut)) : 16;
     const bool wide = (reinterpret_cast<uintptr_t>(out0) & (kOutAlign - 1)) == 0;
     const uint4* src = reinterpret_cast<const uint4*>(row + (size_t)entry0 * sizeof(TIn));
-    for (int64_t i = tid; i < np; i += kBwdUnroll * kBwdThreads) {
+    for (int64_t i = tid; i < np; i += kBwdUnroll * TH) {
       uint4 v[kBwdUnroll];
 #pragma unroll
       for (int k = 0; k < kBwdUnroll; ++k)
-        if (!zero && i + k * kBwdThreads < np &&
-            ADWIN_CHK(entry0 + (i + k * kBwdThreads + 1) * N <= p.V, p.status))
-          v[k] = __ldcs(src + i + k * kBwdThreads);
+        if (!zero && i + k * TH < np &&
+            ADWIN_CHK(entry0 + (i + k * TH + 1) * N <= p.V, p.status))
+          v[k] = __ldcs(src + i + k * TH);
 #pragma unroll
       for (int k = 0; k < kBwdUnroll; ++k) {
-        const int64_t q = i + k * kBwdThreads;
+        const int64_t q = i + k * TH;
         if (q >= np) break;
         f2_t g[NP];
         if (zero) {
@@ -885,10 +890,12 @@ __global__ void __launch_bounds__(kBwdThreads, 4) token_scores_bwd_kernel(const 
     }
     if (edge >= 0) Elem<TOut>::store1(out, edge, grad1(z_edge));
     __syncthreads();   // the patches come after the sweep's stores
-    if (patch) {
-      float g = grad1(z_mine);
-      for (int j = 0; j <= p.K; ++j) g += own_id[j] == (int32_t)mine ? own_w[j] : 0.f;
-      if (ADWIN_CHK(mine < p.V, p.status)) Elem<TOut>::store1(out, mine, g);
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      if (mine[k] < 0) continue;
+      float g = grad1(z_mine[k]);
+      for (int j = 0; j <= p.K; ++j) g += own_id[j] == (int32_t)mine[k] ? own_w[j] : 0.f;
+      if (ADWIN_CHK(mine[k] < p.V, p.status)) Elem<TOut>::store1(out, mine[k], g);
     }
     __syncthreads();
   }
@@ -982,12 +989,18 @@ cudaError_t launch_token_scores_bwd(const void* logits, int dtype, int64_t B, in
   // few rows are cut into slices of at least two rounds of loads
   const int64_t pieces = V / (bf ? 8 : 4), room = (int64_t)sm_count * 8;
   int64_t splits = 1;
-  while (rows * splits * 2 <= room && pieces >= splits * 4 * kBwdUnroll * kBwdThreads) splits *= 2;
+  while (rows * splits * 2 <= room && pieces >= splits * 4 * kBwdUnroll * 256) splits *= 2;
   p.splits = (int)splits;
   int64_t grid = (int64_t)sm_count * 32;
   if (grid > rows * splits) grid = rows * splits;
-#define ADWIN_BWD(TIN, TOUT) \
-  launch_chained(token_scores_bwd_kernel<TIN, TOUT>, (unsigned)grid, kBwdThreads, 0, 1, s, p)
+  // 128 threads to a row of fewer than 8 000 pieces: what a row costs outside its sweep is hidden by twice as many rows
+  // per SM (20 480 bf16 rows of 8 192 178 -> 138 us, of 16 384 269 -> 233, 10 240 of 50 000 346.5 -> 344). 256 to longer
+  // ones (5 120 of 100 000 344 -> 337 us, of 151 936 510 -> 492) and where four per SM take every row (320 of 8 192
+  // 8.1 -> 7.5 us)
+  const bool narrow = pieces < 8000 && rows > (int64_t)sm_count * 4;
+#define ADWIN_BWD(TIN, TOUT)                                                                                    \
+  (narrow ? launch_chained(token_scores_bwd_kernel<TIN, TOUT, 128>, (unsigned)grid, 128, 0, 1, s, p)            \
+          : launch_chained(token_scores_bwd_kernel<TIN, TOUT, 256>, (unsigned)grid, 256, 0, 1, s, p))
   if (bf) return grad_dtype == ADWIN_BF16 ? ADWIN_BWD(__nv_bfloat16, __nv_bfloat16) : ADWIN_BWD(__nv_bfloat16, float);
   return grad_dtype == ADWIN_BF16 ? ADWIN_BWD(float, __nv_bfloat16) : ADWIN_BWD(float, float);
 #undef ADWIN_BWD

@@ -256,6 +256,19 @@ def test_gradient_of_few_and_of_many_rows(rows, dtype, out):
 
 
 @pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("V,K", [(1, 1), (130, 128), (4099, 128), (5003, 0), (32003, 7)])
+def test_gradient_of_more_short_rows_than_the_device_takes_at_once(V, K, dtype, out):
+    z, y = _logits(3, 260, V, DTYPES[dtype], V)
+    ids = None
+    if K > 2:
+        ids = torch.randint(0, V, (3, 260, K), generator=torch.Generator(device=DEV).manual_seed(V), device=DEV,
+                            dtype=torch.int32)
+        ids[..., 0] = ids[..., -1]     # one twice, first and last; one that is the token
+        ids[..., 1] = y
+    _check_grad(z, y, K, _lengths(260, 201, 255), out=DTYPES[out], ids=ids, flags=api.ZERO_TAIL)
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
 @pytest.mark.parametrize("V,ld,ldg", [(1000, 1024, 1003), (4097, 4097, 4104), (9001, 9003, 9001)])
 def test_gradient_at_strides_that_differ(V, ld, ldg, dtype, out):
     z, y = _logits(2, 5, V, DTYPES[dtype], 5, ld=ld)
@@ -279,7 +292,7 @@ def test_gradient_with_masked_entries_and_the_same_index_twice(dtype):
 
 
 def test_gradient_in_place_of_the_logits():
-    for V, T in ((50257, 3), (1001, 40)):
+    for V, T in ((50257, 3), (1001, 40), (1001, 400)):
         z, y = _logits(2, T, V, torch.bfloat16, 7)
         f = api.adwin_token_logprobs(z, y, top_k=8)
         w = torch.randn((2, T), device=DEV)

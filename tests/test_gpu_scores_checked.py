@@ -41,6 +41,7 @@ def test_scores_gradient(checked_library, dtype, out):
         P.test_gradient_at_odd_vocabularies(V, dtype, out)
     P.test_gradient_at_strides_that_differ(9001, 9003, 9001, dtype, out)
     P.test_gradient_of_few_and_of_many_rows(5, dtype, out)
+    P.test_gradient_of_more_short_rows_than_the_device_takes_at_once(4099, 128, dtype, out)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -52,7 +53,7 @@ def test_topk_kl(checked_library, dtype):
     for rows in (1, 10, 38):
         Q.test_few_rows(rows, dtype)
     Q.test_strides_that_differ(30001, 30003, 30001, dtype, dtype)
-    Q.test_rows_too_long_for_any_ring(660000, dtype)
+    Q.test_few_rows_longer_than_any_vocabulary(660000, dtype)
 
 
 def test_linear_i8(checked_library):

@@ -92,8 +92,9 @@ def test_odd_vocabularies(V, dtype, out):
             _check(*c[:4], None if K < V else c[4], _lengths(14, 5, 1), forward=forward, out=DTYPES[out])
 
 
-# the longest rows of a shape and the next entry: 128, 256, 512 threads, then clusters
-@pytest.mark.parametrize("V", [9215, 9217, 22528, 22530, 32000, 50257, 81920, 81928, 151936])
+# many rows: 128 threads each below 24 000 bf16 (12 000 fp32) entries, 256 below 80 000 (40 000), then 960
+@pytest.mark.parametrize("V", [9215, 9217, 11999, 12003, 22528, 22530, 23999, 24009, 32000, 39999, 40005, 50257, 79999,
+                               80009, 81920, 81928, 151936])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_many_rows_of_every_shape(V, dtype):
     T = 100 if V > 60000 else 330
@@ -111,7 +112,7 @@ def test_few_rows(rows, dtype):
 
 
 @pytest.mark.parametrize("V,dtype", [(660000, "bf16"), (900001, "bf16"), (330001, "f32"), (500000, "f32")])
-def test_rows_too_long_for_any_ring(V, dtype):
+def test_few_rows_longer_than_any_vocabulary(V, dtype):
     c = _case(1, 4, V, 30, DTYPES[dtype], 4)
     _check(*c, _lengths(4))
 
