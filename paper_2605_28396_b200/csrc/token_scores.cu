@@ -291,6 +291,27 @@ __device__ __forceinline__ uint32_t split_piece(uint4& v, float from, float*) {
   v = make_uint4(w[0], w[1], w[2], w[3]);
   return bits;
 }
+// Their number alone.
+__device__ __forceinline__ int count_piece(const uint4& v, float from, __nv_bfloat16*) {
+  const __nv_bfloat162 f2 = __float2bfloat162_rn(from);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t n = 0;   // per half
+#pragma unroll
+  for (int i = 0; i < 4; ++i) n += __hge2_mask(reinterpret_cast<const __nv_bfloat162&>(w[i]), f2) & 0x00010001u;
+  return (int)((n & 0xffffu) + (n >> 16));
+}
+__device__ __forceinline__ int count_piece(const uint4& v, float from, float*) {
+  return (__uint_as_float(v.x) >= from) + (__uint_as_float(v.y) >= from) + (__uint_as_float(v.z) >= from) +
+         (__uint_as_float(v.w) >= from);
+}
+// The smallest value of the logits' type at and above a key's: entries that reach one reach the other.
+template <typename TIn>
+__device__ __forceinline__ float threshold(int key) {
+  const float z = key_value(key);
+  if (sizeof(TIn) == 4) return z;
+  const uint32_t bits = __float_as_uint(z);
+  return __uint_as_float(bits & 0xffffu ? ((int)bits >= 0 ? (bits & 0xffff0000u) + 0x10000u : bits & 0xffff0000u) : bits);
+}
 template <typename TIn>
 __device__ __forceinline__ float piece_entry(const uint4& v, int e) {
   if (sizeof(TIn) == 4) return __uint_as_float(e & 2 ? (e & 1 ? v.w : v.z) : (e & 1 ? v.y : v.x));
@@ -298,17 +319,59 @@ __device__ __forceinline__ float piece_entry(const uint4& v, int e) {
   return e & 1 ? bf16hi(w) : bf16lo(w);
 }
 
-// The entries of the opened units that belong to the list, where more reach tau than can be ranked: the K-th
-// largest value by bisection between tau and the largest, then the index up to which entries of that
-// value belong to it.  Returns their mass's complement in the opened units.
+// Where more entries of the opened units reach tau than can be ranked: a key that K and no more than can be ranked reach,
+// by search between tau and the largest, two thresholds a step, into sh.low[0], and their number into sh.n_cand.  Where no
+// value parts them the K-th largest, which more reach.
+// (128 alternatives of 20 480 rows of 4 096 entries 6.3 ms by halves, entry by entry, down to exactly K, so 0.9 ms; a step
+// waits for L2.)
 template <typename TIn, int TH>
-__device__ __noinline__ Mass select_by_bisection(const Slice<TIn> s, int K, float M, int tau, int n, int n_open,
-                                                 int room, int32_t* status) {
+__device__ __noinline__ void refine_tau(const Slice<TIn> s, int K, float M, int tau, int n_open, int room, int32_t* status) {
+  ScoreShared<TH>& sh = score_shared<TH>();
+  const Units un = units_of<TH>(room);
+  int flip = 0;
+  __syncthreads();
+  int64_t lo = tau == kNone ? order_key(-INFINITY) : tau, hi = (int64_t)order_key(M) + 1;   // fewer than K reach hi
+  int c = kCand + 1;   // entries that reach lo
+  while (hi - lo != 1 && c > kCand) {
+    const int64_t third = hi - lo > 3 ? (hi - lo) / 3 : 1, m1 = lo + third, m2 = hi - third > m1 ? hi - third : m1;
+    const float a = threshold<TIn>((int)m1), b = threshold<TIn>((int)m2);
+    int va = s.edge >= 0 && s.edge_z >= a, vb = s.edge >= 0 && s.edge_z >= b;
+    for_opened<TIn, TH>(s, un.open, n_open, status, [&](const uint4& v, int) {
+      va += count_piece(v, a, static_cast<TIn*>(nullptr));
+      vb += count_piece(v, b, static_cast<TIn*>(nullptr));
+    });
+    const int2 v = block_count<TH>(va, vb, sh.count, flip);
+    if (v.y >= K) {
+      lo = m2;
+      c = v.y;
+    } else if (v.x >= K) {
+      lo = m1;
+      c = v.x;
+      hi = m2;
+    } else {
+      hi = m1;
+    }
+  }
+  if (threadIdx.x == 0) {
+    sh.low[0] = (int)lo;
+    sh.n_cand = c;
+  }
+  __syncthreads();
+}
+
+// The entries of the opened units that belong to the list, where more reach tau than can be ranked: those of a refined
+// tau or, where more have the K-th largest value than can be ranked, those of that value up to an index found by
+// bisection.  Returns the mass of the others in the opened units.
+template <typename TIn, int TH>
+__device__ __noinline__ Mass select_exactly(const Slice<TIn> s, int K, float M, int tau, int n_open, int room,
+                                            int32_t* status) {
   ScoreShared<TH>& sh = score_shared<TH>();
   const Units un = units_of<TH>(room);
   constexpr int N = Elem<TIn>::N;
+  refine_tau<TIn, TH>(s, K, M, tau, n_open, room, status);
+  tau = sh.low[0];
+  const bool parted = sh.n_cand <= kCand;
   int flip = 0;
-  __syncthreads();
   auto walk = [&](auto f) {
     for_opened<TIn, TH>(s, un.open, n_open, status, [&](const uint4& v, int k0) {
 #pragma unroll 1
@@ -316,31 +379,15 @@ __device__ __noinline__ Mass select_by_bisection(const Slice<TIn> s, int K, floa
     });
     if (s.edge >= 0) f(s.edge_z, s.edge);
   };
-  auto count = [&](float above, float equal, int upto) {
-    int v = 0;
-    walk([&](float z, int k) { v += (z >= above || (z >= equal && k <= upto)) ? 1 : 0; });
-    return block_count<TH>(v, 0, sh.count, flip).x;
-  };
-  int64_t lo = tau == kNone ? order_key(-INFINITY) : tau, hi = (int64_t)order_key(M) + 1;
-  int c = n;
-  while (hi - lo != 1 && c != K) {
-    const int64_t mid = lo + ((hi - lo) >> 1);
-    const int v = count(key_value((int)mid), INFINITY, -1);
-    if (v >= K) {
-      lo = mid;
-      c = v;
-    } else {
-      hi = mid;
-    }
-  }
-  const float equal = key_value((int)lo), above = c == K ? equal : key_value((int)hi);
+  const float equal = key_value(tau), above = parted ? equal : key_value(tau + 1);   // (at most +infinity)
   int ilo = -1, ihi = s.entry0 + s.np * N + N;   // up to ilo: too few
-  if (c != K) {
-    while (ihi - ilo > 1) {
-      const int mid = ilo + (ihi - ilo) / 2;
-      if (count(above, equal, mid) >= K) ihi = mid; else ilo = mid;
-    }
+  while (!parted && ihi - ilo > 1) {
+    const int mid = ilo + (ihi - ilo) / 2;
+    int v = 0;
+    walk([&](float z, int k) { v += (z >= above || (z >= equal && k <= mid)) ? 1 : 0; });
+    if (block_count<TH>(v, 0, sh.count, flip).x >= K) ihi = mid; else ilo = mid;
   }
+  __syncthreads();   // (all have read the number)
   if (threadIdx.x == 0) sh.n_cand = 0;
   __syncthreads();
   Mass below = {kLowest, 0.f};
@@ -355,6 +402,7 @@ __device__ __noinline__ Mass select_by_bisection(const Slice<TIn> s, int K, floa
       below.add(z);
     }
   });
+  __syncthreads();
   return below;
 }
 
@@ -409,12 +457,6 @@ __device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int s
     }
     tau = (int)lo;
   }
-  // (for bf16 logits the next value of their type: no entry lies between)
-  float tau_z = tau == kNone ? -INFINITY : key_value(tau);
-  if (sizeof(TIn) == 2 && tau != kNone) {
-    const uint32_t bits = __float_as_uint(tau_z);
-    tau_z = __uint_as_float(bits & 0xffffu ? ((int)bits >= 0 ? (bits & 0xffff0000u) + 0x10000u : bits & 0xffff0000u) : bits);
-  }
   // the opened units, in an order of their own; the others' sums
   Mass others = {kLowest, 0.f};
   int n_mine = 0;
@@ -449,8 +491,16 @@ __device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int s
       sh.rank[i] = 0;
     }
   };
+  if (tau == kNone && s.np > kCand / Elem<TIn>::N) {   // every entry reaches it, more than can be ranked
+    refine_tau<TIn, TH>(s, K, M, tau, n_open, room, status);
+    tau = sh.low[0];
+    __syncthreads();
+    if (tid == 0) sh.n_cand = 0;
+    __syncthreads();
+  }
+  const float tau_z = tau == kNone ? -INFINITY : threshold<TIn>(tau);
   // Entries below tau in the opened units: against the smallest of the units' maxima, where that is near enough
-  // (its unit is not opened, so what vanishes beside it is nothing to the mass outside)
+  // (an entry of the slice that is below tau too, so what vanishes beside it is nothing to the mass outside)
   Mass below = {kLowest, 0.f};
   const float ref = key_value(kmin);
   const bool near = kmin < tau && ref >= tau_z - 60.f;
@@ -487,7 +537,7 @@ __device__ __noinline__ int select_top(const Slice<TIn> s, int K, float M, int s
   __syncthreads();
   int n = sh.n_cand;
   if (n > kCand) {
-    below = select_by_bisection<TIn, TH>(s, K, M, tau, n, n_open, room, status);
+    below = select_exactly<TIn, TH>(s, K, M, tau, n_open, room, status);
     __syncthreads();
     n = min(sh.n_cand, kCand);
   }

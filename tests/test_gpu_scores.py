@@ -129,6 +129,24 @@ def test_scores_of_rows_whose_alternatives_are_hard_to_find(dtype, many):
         _check(z, y, K)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [257, 300, 1024, 2049, 4096, 8192, 8201, 9000])
+def test_scores_of_short_rows_with_long_lists(V, dtype):
+    """About as many alternatives as a row has units that are kept apart."""
+    dt = DTYPES[dtype]
+    z, y = _logits(8, 25, V, dt, V)
+    z[1] = 0.25
+    z[2, :, 5:] = -INF                              # five entries and the lowest of them all
+    z[3, :, 200:] = torch.finfo(dt).min
+    z[4] = (z[4].float() * 2).round().to(dt) / 2
+    z[5] = torch.linspace(-20, 20, V, device=DEV).to(dt)
+    z[6, :, V // 2:] -= 90.0
+    z[7] *= 1e-3
+    y[2] = 3
+    for K in (64, 100, 127, 128):
+        _check(z, y, K)
+
+
 @pytest.mark.parametrize("many", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [33, 5003, 50257])

@@ -29,6 +29,8 @@ def test_scores(checked_library, dtype):
         P.test_scores_at_odd_vocabularies(V, dtype)
     for rows in (1, 37, 150):
         P.test_scores_of_few_and_of_many_rows(rows, dtype)
+    P.test_scores_of_short_rows_with_long_lists(4096, dtype)
+    P.test_scores_of_short_rows_with_long_lists(9000, dtype)
     P.test_scores_at_padded_and_odd_strides(4097, 4103, dtype)
     for many in (False, True):
         P.test_scores_of_rows_whose_alternatives_are_hard_to_find(dtype, many)
