@@ -233,7 +233,11 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       const int64_t m0 = (int64_t)(2 * pm + (int)rank) * kBM + quad * 32, n0 = (int64_t)nt * kBN + half * 128;
       const int rows = p.M - m0 < 32 ? (p.M > m0 ? (int)(p.M - m0) : 0) : 32;
       const int cols = p.N - n0 < 128 ? (p.N > n0 ? (int)(p.N - n0) : 0) : 128;
+      // (the steps are asked for while the tile is on its way)
       const float sx = lane < rows ? __ldg(p.step_x + m0 + lane) : 0.f;
+      float steps[4];   // of columns lane, 32 + lane, ...
+#pragma unroll
+      for (int j = 0; j < 4; ++j) steps[j] = j * 32 + lane < cols ? __ldg(p.step_w + n0 + j * 32 + lane) : 0.f;
       if (!__all_sync(0xffffffffu, bar_wait(smem_addr(&ctrl->acc_full[slot]), aph, abort, p.limit_ns))) break;
       tc_fence_after_sync();
       const uint32_t t_lane = tmem_base + ((uint32_t)(quad * 32) << 16) + slot * kBN + (uint32_t)(half * 128);
@@ -246,8 +250,7 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
           uint32_t r[32];
           tmem_ld32(t_lane + pass * kPass + j * 32, r);
           tmem_ld_wait();
-          const int c0 = pass * kPass + j * 32;
-          const float sw = c0 + lane < cols ? __ldg(p.step_w + n0 + c0 + lane) : 0.f;   // column c0 + lane's
+          const float sw = pass == 0 ? steps[j] : steps[2 + j];
           constexpr int kUnit = 16 / (int)sizeof(TOut);   // results of a 16-byte unit
 #pragma unroll
           for (int u = 0; u < 32 / kUnit; ++u) {
