@@ -421,7 +421,8 @@ int adwin_opd_kl_fwd_bwd_no_alloc(const void* student_logits, const void* teache
  *                                                 order of their index
  *   rest[b,t]     = log of the mass outside them  (-inf where there is none)
  * Other positions get 0, in top_ids -1.  Sums are fp32; rest is summed over the entries outside the
- * list, not taken from 1, so that it keeps its relative precision however small the mass is.
+ * list, not taken from 1, so that it keeps its relative precision however small the mass is; where the
+ * list holds less than half it is log1p(-the list's), so that rest itself does however near 0 it is.
  *
  * logits       : [B,T,V], element type `dtype`, row stride ld >= V elements, any alignment
  * tokens       : [B,T] int32;  window, rollout_len: [B] int32 or NULL (= T)

@@ -14,7 +14,8 @@
 // K of them, a few KB that are still in L2.  Their entries >= tau, about K again, are ranked against one
 // another (larger first, then lower index).  The mass outside is the sum over the units that were
 // not opened, the entries below tau in those that were, and the losers: all terms positive, so it
-// keeps its relative precision however small it is (as 1 - sum of the list it would not).  A row with
+// keeps its relative precision however small it is (as 1 - sum of the list it would not); where the list holds less
+// than half, its log is made of the list all the same: near 0 that has no rounding of the sums' size in it.  A row with
 // more than kCand entries >= tau (long ties, sorted rows) has its threshold found by bisection, on
 // the value and then on the index, over the opened units.  Nothing depends on the order of atomics:
 // the candidates' ranks do not, and sums run in the order of ranks and units.
@@ -775,11 +776,18 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
           p.top_logprobs[r * K + j] = finite ? (sh.sorted_z[j] - tot.m) - ln_s : nan;
         }
       }
+      float listed = 1.f;   // the list's share, where it is less than half
+      if (TOP && tid < 32 && finite) {
+        float w = 0.f;
+        for (int j = tid; j < K; j += 32) w += ex2f((sh.sorted_z[j] - tot.m) * kLog2e);
+        listed = lane_sum(w) / tot.s;
+      }
       if (tid == 0) {
         p.logprob[r] = (y_valid && finite) ? (zy - tot.m) - ln_s : nan;
         if (p.entropy) p.entropy[r] = finite ? fmaf(-tot.a / tot.s, kLn2, ln_s) : nan;
         if (p.lse) p.lse[r] = lse;
-        if (p.rest) p.rest[r] = finite ? (rest.m - tot.m) + (logf(rest.s) - ln_s) : nan;
+        if (TOP && p.rest)
+          p.rest[r] = !finite ? nan : listed < 0.5f ? log1pf(-listed) : (rest.m - tot.m) + (logf(rest.s) - ln_s);
         int bits = 0;
         if (!y_valid) bits |= ADWIN_DEV_TOKEN_RANGE;
         if (!finite) bits |= ADWIN_DEV_NONFINITE;

@@ -147,6 +147,20 @@ def test_scores_of_short_rows_with_long_lists(V, dtype):
         _check(z, y, K)
 
 
+@pytest.mark.parametrize("rows", [1, 200])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_mass_outside_short_lists_of_flat_rows(dtype, rows):
+    """rest = log(1 - q) near 0.  q has the sums' 1e-5 of itself (its exponents, at most 16 here, add
+    16 u), -log(1 - q) is at least q and grows by at most 1 / (1 - q) < 2 per unit of q: 4e-5 of itself."""
+    for V, std in ((50257, 0.5), (151936, 1.0), (4099, 0.0)):
+        z, y = _logits(rows, 1, V, DTYPES[dtype], V, std=std)
+        for K in (1, 5, 64):
+            o = api.adwin_token_logprobs(z, y, top_k=K)
+            r = S.scores(z[:, 0], y[:, 0], K)["rest"]
+            assert (r > math.log(0.5)).all()
+            _same(o.rest[:, 0], r, 4e-5 * r.abs(), "rest")
+
+
 @pytest.mark.parametrize("many", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [33, 5003, 50257])

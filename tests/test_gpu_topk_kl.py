@@ -105,6 +105,23 @@ def test_many_rows_of_every_shape(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 200])
+def test_step_cost_of_a_rest_that_is_nearly_everything(dtype, rows):
+    """logratio of tokens outside the list is log P_r where the teacher's is 0: log(1 - q), whose q has the sums'
+    1e-5 and its exponents' 16 u, so 4e-5 of itself while q is less than half."""
+    for V, std in ((50257, 0.5), (151936, 1.0)):
+        z, y, ids, top, rest = _case(rows, 1, V, 5, DTYPES[dtype], V, std=std)
+        y[:] = ids.min() - 1 if int(ids.min()) > 0 else ids.max() + 1
+        assert int(y[0, 0]) < V
+        for forward in (False, True):
+            o = api.adwin_opd_topk_kl_fwd_bwd(z, y, ids, top, _lengths(*[1] * rows), None, rest=torch.zeros_like(rest),
+                                              kl_mode=api.KL_FORWARD if forward else api.KL_REVERSE)
+            r = S.topk_kl(z[:, 0], y[:, 0], ids[:, 0], top[:, 0], torch.zeros_like(rest[:, 0]), forward, 1.0)["logratio"]
+            assert int(o.dev_status.item()) == 0 and (r > math.log(0.5)).all()
+            _same(o.logratio[:, 0], r, 4e-5 * r.abs(), "logratio")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows", [1, 2, 9, 10, 18, 19, 37, 38, 75])
 def test_few_rows(rows, dtype):
     c = _case(rows, 1, 151936, 64, DTYPES[dtype], rows, std=4.0)
