@@ -184,11 +184,7 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
           tma_load_2d_pair(b, &map_w, kb * kBKBytes, n0, bar0);
         }
       }
-      if (!ok && rank == 0) {   // give up: let the copies in flight land
-        const uint32_t n_out = it < (uint32_t)kStages ? it : (uint32_t)kStages;
-        for (uint32_t j = it - n_out; j < it; ++j)
-          bar_wait_drain(smem_addr(&ctrl->full[j % kStages]), (j / kStages) & 1);
-      }
+      pair_issued(ctrl, rank, it);
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
@@ -212,10 +208,6 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
           umma_commit_pair(smem_addr(&ctrl->empty[s]));
         }
         if (ok) umma_commit_pair(smem_addr(&ctrl->acc_full[slot]));
-      }
-      if (!ok) {
-        umma_commit_pair(smem_addr(&ctrl->drain));
-        bar_wait_drain(smem_addr(&ctrl->drain), 0);
       }
     }
   } else if (warp >= kEpiWarp0) {
@@ -298,13 +290,7 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
     atomicOr(p.status, ADWIN_DEV_TIMEOUT);
     store_cluster_u32(map_to_cta(smem_addr(&ctrl->abort), rank ^ 1u), 1u);
   }
-  tc_fence_before_sync();
-  __syncthreads();
-  cluster_sync();
-  if (warp == 2) {
-    tc_fence_after_sync();
-    tmem_dealloc_pair(tmem_base, kTmemCols);
-  }
+  pair_finish<kStages>(ctrl, rank, p.status);
 }
 
 // ---------------------------------------------------------------------------- few rows of x

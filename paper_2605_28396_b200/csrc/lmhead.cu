@@ -453,7 +453,7 @@ lm_sweep_kernel(const __grid_constant__ CUtensorMap map_hs, const __grid_constan
         }
       }
       pace.done();
-      if (!ok && rank == 0) pair_drain_loads(ctrl, it);
+      pair_issued(ctrl, rank, it);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
@@ -479,10 +479,6 @@ lm_sweep_kernel(const __grid_constant__ CUtensorMap map_hs, const __grid_constan
             if (ok) umma_commit_pair(smem_addr(&ctrl->acc_full[pass]));
           }
         }
-      }
-      if (!ok) {   // give up: wait until the MMAs already issued have retired
-        umma_commit_pair(smem_addr(&ctrl->drain));
-        bar_wait_drain(smem_addr(&ctrl->drain), 0);
       }
     }
   } else if (warp >= kEpiWarp0) {
@@ -599,13 +595,7 @@ lm_sweep_kernel(const __grid_constant__ CUtensorMap map_hs, const __grid_constan
     atomicOr(p.status, ADWIN_DEV_TIMEOUT);
     store_cluster_u32(map_to_cta(smem_addr(&ctrl->abort), rank ^ 1u), 1u);   // partner too
   }
-  tc_fence_before_sync();
-  __syncthreads();
-  cluster_sync();   // neither CTA leaves while the other may still use its memory
-  if (warp == 2) {
-    tc_fence_after_sync();
-    tmem_dealloc_pair(tmem_base, kTmemCols);
-  }
+  pair_finish<kPairStages>(ctrl, rank, p.status);
 }
 
 // ---------------------------------------------------------------------------- merge kernel

@@ -233,7 +233,7 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
       }
       pace.done();
-      if (!ok && rank == 0) pair_drain_loads(ctrl, it);
+      pair_issued(ctrl, rank, it);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
@@ -263,10 +263,6 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             bar_arrive_cluster(map_to_cta(smem_addr(&ctrl->acc_full[slot]), 1));
           }
         }
-      }
-      if (!ok) {   // give up: wait until the MMAs already issued have retired
-        umma_commit_pair(smem_addr(&ctrl->drain));
-        bar_wait_drain(smem_addr(&ctrl->drain), 0);
       }
     }
   } else if (warp >= kEpiWarp0) {
@@ -330,13 +326,7 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     atomicOr(p.status, ADWIN_DEV_TIMEOUT);
     store_cluster_u32(map_to_cta(smem_addr(&ctrl->abort), rank ^ 1u), 1u);   // partner too
   }
-  tc_fence_before_sync();
-  __syncthreads();
-  cluster_sync();   // neither CTA leaves while the other may still use its memory
-  if (warp == 2) {
-    tc_fence_after_sync();
-    tmem_dealloc_pair(tmem_base, kTmemCols);
-  }
+  pair_finish<kPairStages>(ctrl, rank, p.status);
 }
 
 // Sums the pieces of the split tiles in order and stores C; a thread owns 8 columns of a row.

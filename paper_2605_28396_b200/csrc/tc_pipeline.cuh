@@ -46,6 +46,7 @@ struct Ctrl {
   unsigned long long acc_full[2];      // MMA -> epilogue: accumulator slot complete
   unsigned long long acc_empty[2];     // epilogue -> MMA: accumulator slot read out
   unsigned long long drain;            // give-up path: all issued MMAs have retired
+  uint32_t issued[2];                  // in the even CTA: k-blocks that each CTA's producer has issued
   uint32_t tmem_base;
   int abort;
 };
@@ -76,6 +77,10 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
 __device__ __forceinline__ void bar_expect_tx(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
                : "memory");
+}
+// Counts bytes as arrived without a copy, for one that will never be issued.
+__device__ __forceinline__ void bar_complete_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ bool bar_try_wait(uint32_t bar, uint32_t parity) {
   uint32_t ok;
@@ -335,12 +340,63 @@ __device__ __forceinline__ void pair_release(unsigned long long* acc_empty, uint
   if (rank != 0) bar_arrive_cluster(map_to_cta(smem_addr(acc_empty), 0));
   else bar_arrive(smem_addr(acc_empty));
 }
-// Give-up path of the even CTA's producer after `it` k-blocks: let the copies in flight land (its
-// barriers count both CTAs' bytes; the final cluster barrier holds the odd CTA meanwhile).
-__device__ __forceinline__ void pair_drain_loads(Ctrl* ctrl, uint32_t it) {
-  const uint32_t n_out = it < (uint32_t)kPairStages ? it : (uint32_t)kPairStages;
-  for (uint32_t j = it - n_out; j < it; ++j)
-    bar_wait_drain(smem_addr(&ctrl->full[j % kPairStages]), (j / kPairStages) & 1);
+// A producer's last act: the even CTA learns how many k-blocks it has issued.
+__device__ __forceinline__ void pair_issued(Ctrl* ctrl, uint32_t rank, uint32_t it) {
+  store_cluster_u32(map_to_cta(smem_addr(&ctrl->issued[rank]), 0), it);
+}
+// Give-up path, one thread of the even CTA, once both producers have ended: let the copies in flight
+// land.  Its `full` barriers count both CTAs' bytes, and the producers may have stopped at different
+// k-blocks: bytes that never come are counted as there, bytes that it has not announced are.
+// (`empty` lets a producer take stage s for k-block j only when j - kStages has been consumed in both CTAs, so
+// the barrier is in k-block j's phase, and the counts differ by kStages at most.)
+template <int kStages>
+__device__ __forceinline__ void pair_drain_loads(Ctrl* ctrl) {
+  const uint32_t even = ctrl->issued[0], odd = ctrl->issued[1];
+  const uint32_t most = even > odd ? even : odd;
+  for (uint32_t j = even < odd ? even : odd; j < most; ++j) {
+    const uint32_t bar = smem_addr(&ctrl->full[j % kStages]);
+    if (even > odd) bar_complete_tx(bar, kPairStageBytes);
+    else bar_expect_tx(bar, kPairStageBytes);
+  }
+  const uint32_t n_out = most < (uint32_t)kStages ? most : (uint32_t)kStages;
+  for (uint32_t j = most - n_out; j < most; ++j)
+    bar_wait_drain(smem_addr(&ctrl->full[j % kStages]), (j / kStages) & 1);
+}
+// Whether no copy is in flight any more (every byte of the last k-blocks has been counted).
+template <int kStages>
+__device__ __forceinline__ bool pair_landed(Ctrl* ctrl) {
+  const uint32_t most = ctrl->issued[0] > ctrl->issued[1] ? ctrl->issued[0] : ctrl->issued[1];
+  const uint32_t n_out = most < (uint32_t)kStages ? most : (uint32_t)kStages;
+  for (uint32_t j = most - n_out; j < most; ++j)
+    if (!bar_test_wait(smem_addr(&ctrl->full[j % kStages]), (j / kStages) & 1)) return false;
+  return true;
+}
+// End of a pair kernel, all threads of both CTAs.  A wait that ran out in one role leaves the others
+// where they were: the producers may have issued all their copies, the issuer all its MMAs.  So what
+// is in flight is waited for here, whichever role gave up, before shared and tensor memory go.
+template <int kStages>
+__device__ __forceinline__ void pair_finish(Ctrl* ctrl, uint32_t rank, int32_t* status) {
+  volatile int* abort = &ctrl->abort;
+  tc_fence_before_sync();
+  __syncthreads();   // this CTA's roles have ended
+  if (threadIdx.x == 0 && *abort) store_cluster_u32(map_to_cta(smem_addr(&ctrl->abort), rank ^ 1u), 1u);
+  cluster_sync();    // neither CTA leaves while the other may still use its memory
+  if (*abort) {      // (the same in both)
+    if (threadIdx.x == 32) {   // the thread that issued the MMAs; the commit reaches both CTAs
+      if (rank == 0) umma_commit_pair(smem_addr(&ctrl->drain));
+      bar_wait_drain(smem_addr(&ctrl->drain), 0);
+    }
+    if (threadIdx.x == 0 && rank == 0) pair_drain_loads<kStages>(ctrl);
+    __syncthreads();
+    cluster_sync();
+  }
+#ifdef ADWIN_CHECKED
+  if (threadIdx.x == 0 && rank == 0 && !pair_landed<kStages>(ctrl)) atomicOr(status, (int32_t)ADWIN_DEV_BOUNDS);
+#endif
+  if ((threadIdx.x >> 5) == 2) {
+    tc_fence_after_sync();
+    tmem_dealloc_pair(ctrl->tmem_base, kTmemCols);
+  }
 }
 
 }  // namespace tc
