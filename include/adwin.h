@@ -101,8 +101,8 @@ int adwin_version(void);
  * memory and returns; the outputs of that call are invalid, the context stays usable.  This sets
  * the limit of those handshake waits for the launches that follow, process-wide, in nanoseconds
  * (default 2 s; 0 restores the default).  A limit below 16 ns makes every wait that is not
- * satisfied at the moment it is reached run out, which is how the tests exercise the give-up path; there
- * is no other use for it.  The paper has no counterpart.
+ * satisfied at the moment it is reached run out, and the tensor-core kernels keep to limits below 0.1 ms to
+ * within a look at the clock, which is how the tests exercise the give-up paths; there is no other use for it.  The paper has no counterpart.
  */
 void adwin_diag_set_wait_limit_ns(uint64_t ns);
 

@@ -286,10 +286,6 @@ linear_i8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       if (lane == 0) pair_release(&ctrl->acc_empty[slot], rank);
     }
   }
-  if (*abort && threadIdx.x == 0) {
-    atomicOr(p.status, ADWIN_DEV_TIMEOUT);
-    store_cluster_u32(map_to_cta(smem_addr(&ctrl->abort), rank ^ 1u), 1u);
-  }
   pair_finish<kStages>(ctrl, rank, p.status);
 }
 

@@ -591,10 +591,6 @@ lm_sweep_kernel(const __grid_constant__ CUtensorMap map_hs, const __grid_constan
       }
     }
   }
-  if (*abort && threadIdx.x == 0) {
-    atomicOr(p.status, ADWIN_DEV_TIMEOUT);
-    store_cluster_u32(map_to_cta(smem_addr(&ctrl->abort), rank ^ 1u), 1u);   // partner too
-  }
   pair_finish<kPairStages>(ctrl, rank, p.status);
 }
 

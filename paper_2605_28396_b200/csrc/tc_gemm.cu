@@ -322,10 +322,6 @@ tc_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       if (lane == 0) pair_release(&ctrl->acc_empty[slot], rank);
     }
   }
-  if (*abort && threadIdx.x == 0) {
-    atomicOr(p.status, ADWIN_DEV_TIMEOUT);
-    store_cluster_u32(map_to_cta(smem_addr(&ctrl->abort), rank ^ 1u), 1u);   // partner too
-  }
   pair_finish<kPairStages>(ctrl, rank, p.status);
 }
 

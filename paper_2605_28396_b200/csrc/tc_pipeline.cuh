@@ -20,6 +20,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../../include/adwin.h"
+
 namespace adwin {
 namespace tc {
 
@@ -37,6 +39,7 @@ constexpr int kThreads = 384;       // warp 0: TMA producer, warp 1: MMA issuer,
 constexpr int kEpiWarp0 = 4;
 constexpr int kEpiThreads = 256;
 constexpr uint64_t kWaitLimitNs = 2000000000ull;  // 2 s
+constexpr uint64_t kShortLimitNs = 100000ull;     // limits that try_wait, which may suspend the thread, would not keep
 
 // Control block at the start of dynamic shared memory; the stages follow at the next 1024-byte
 // boundary.
@@ -110,10 +113,16 @@ __device__ __forceinline__ bool bar_test_wait(uint32_t bar, uint32_t parity) {
 // raises the CTA's abort flag.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort,
                                          uint64_t limit_ns = kWaitLimitNs) {
-  if (limit_ns < 16) {   // diagnostic setting: a wait that is not satisfied right now runs out
-    if (bar_test_wait(bar, parity)) return true;
-    *abort = 1;
-    return false;
+  if (limit_ns < kShortLimitNs) {   // diagnostic setting; below 16, a wait that is not satisfied right now runs out
+    const uint64_t t0 = limit_ns < 16 ? 0 : timer_ns();
+    for (;;) {
+      if (bar_test_wait(bar, parity)) return true;
+      if (limit_ns >= 16 && *abort) return false;
+      if (limit_ns < 16 || timer_ns() - t0 > limit_ns) {
+        *abort = 1;
+        return false;
+      }
+    }
   }
   if (bar_try_wait(bar, parity)) return true;
   if (*abort) return false;
@@ -372,16 +381,19 @@ __device__ __forceinline__ bool pair_landed(Ctrl* ctrl) {
   return true;
 }
 // End of a pair kernel, all threads of both CTAs.  A wait that ran out in one role leaves the others
-// where they were: the producers may have issued all their copies, the issuer all its MMAs.  So what
-// is in flight is waited for here, whichever role gave up, before shared and tensor memory go.
+// where they were: the producers may have issued all their copies, the issuer all its MMAs.  So it is reported,
+// and what is in flight waited for, here, whichever role gave up, before shared and tensor memory go.
 template <int kStages>
 __device__ __forceinline__ void pair_finish(Ctrl* ctrl, uint32_t rank, int32_t* status) {
   volatile int* abort = &ctrl->abort;
+  // (the partner need not wait any longer either)
+  if (threadIdx.x == 0 && *abort) store_cluster_u32(map_to_cta(smem_addr(&ctrl->abort), rank ^ 1u), 1u);
   tc_fence_before_sync();
-  __syncthreads();   // this CTA's roles have ended
+  __syncthreads();   // this CTA's roles have ended: only now is it known whether one of them gave up
   if (threadIdx.x == 0 && *abort) store_cluster_u32(map_to_cta(smem_addr(&ctrl->abort), rank ^ 1u), 1u);
   cluster_sync();    // neither CTA leaves while the other may still use its memory
   if (*abort) {      // (the same in both)
+    if (threadIdx.x == 0) atomicOr(status, (int32_t)ADWIN_DEV_TIMEOUT);
     if (threadIdx.x == 32) {   // the thread that issued the MMAs; the commit reaches both CTAs
       if (rank == 0) umma_commit_pair(smem_addr(&ctrl->drain));
       bar_wait_drain(smem_addr(&ctrl->drain), 0);
