@@ -507,7 +507,8 @@ int adwin_opd_topk_kl_fwd_bwd(const void* student_logits, int dtype, int64_t B, 
  * Rows to 8 bits with a step each: the activations of a product in 8-bit integers (a step per token), and,
  * once, its weights (a step per output channel).
  *   scale[i] = max_k |x[i,k]| / 127,   q[i,k] = x[i,k] / scale[i] rounded to the nearest whole number, ties
- *   to even, both divisions correctly rounded in fp32;   q = 0 where scale is 0
+ *   to even, both divisions correctly rounded in fp32;   q = 0 where scale is 0,   and |q| <= 127: where
+ *   the scale is so few units of 2^-149 (fp32 rows below 2.3e-41) that rounding it left it too small, larger quotients end there
  * x            : [M,d], element type `dtype`, row stride ldx >= d elements, any alignment
  * q            : [M,d] int8, row stride ldq >= d bytes (multiples of 16 for adwin_linear_i8); bytes
  *                behind a row's d are left as they are

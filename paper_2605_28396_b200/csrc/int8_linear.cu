@@ -1,8 +1,8 @@
 // Products in 8-bit integers: rows quantised with a step each, and out = (x w^T) in whole numbers times the
 // two rows' steps.  It is the output projection of a frozen policy whose embedding is kept in 8 bits.
 //
-// quantize_rows_kernel:  step = max|x| / 127,  q = x / step to the nearest whole number, ties to even,
-// both divisions correctly rounded in fp32, so that every implementation of this definition gets the same q.
+// quantize_rows_kernel:  step = max|x| / 127,  q = x / step to the nearest whole number, ties to even, within
+// [-127, 127], both divisions correctly rounded in fp32, so that every implementation of this definition gets the same q.
 //
 // linear_i8_few_kernel (up to 16 rows of x): one pass over w, memory-bound; see there.
 //
@@ -38,7 +38,10 @@ struct QuantParams {
   int32_t* status;
 };
 
-__device__ __forceinline__ int quantized(float x, float step) { return __float2int_rn(__fdiv_rn(x, step)); }
+// (a subnormal step is rounded by up to half a unit of 2^-149: the largest entry may be more than 127 of it)
+__device__ __forceinline__ int quantized(float x, float step) {
+  return max(-127, min(127, __float2int_rn(__fdiv_rn(x, step))));
+}
 
 template <typename TIn>
 __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const QuantParams p) {

@@ -166,3 +166,23 @@ def test_an_8_bit_teacher_scores_a_rollout():
     ref = S.topk_kl(z[mask], y[mask], t.top_ids[mask], t.top_logprobs[mask], t.rest[mask], False)
     assert int(o.dev_status.item()) == 0
     assert ((o.kl[mask].double() - ref["kl"]).abs() <= 3e-5 * (1 + ref["size_kl"])).all()
+
+
+@pytest.mark.parametrize("d", [1, 7, 16, 1000, 1003])
+def test_rows_whose_step_is_a_few_units_of_the_smallest_number(d):
+    """A subnormal step is rounded by up to half a unit: max / step may pass 127 (190 units: step 1), and ends
+    at 127 with its sign.  Values and steps are whole numbers of units, formed here in 64 bits."""
+    unit = 2.0 ** -149
+    tops = [1, 63, 64, 100, 127, 128, 143, 190, 191, 254, 316, 444, 1000, 4321, 16000, 16129, 32767, 1 << 20]
+    g = torch.Generator().manual_seed(d)
+    k = torch.stack([torch.randint(-m, m + 1, (d,), generator=g) for m in tops]).double()
+    for i, m in enumerate(tops):
+        k[i, (d // 2 + i) % d] = m if i % 2 else -m
+    x = (k * unit).float()
+    assert torch.equal(x.double() / unit, k)                     # (no flush on the way)
+    q, scale = api.adwin_quantize_rows_i8(x.to(DEV))
+    step = torch.round(k.abs().amax(dim=1) / 127)                # (no quotient lies half way: 127 is odd)
+    assert torch.equal(scale.cpu().double() / unit, step)
+    ratio = (k / step[:, None].clamp(min=1)).float().double()    # rounded to fp32 as the definition does
+    want = torch.where(step[:, None] > 0, torch.round(ratio).clamp(-127, 127), torch.zeros_like(k))
+    assert torch.equal(q.cpu().double(), want)
