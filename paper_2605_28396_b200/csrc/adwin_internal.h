@@ -35,6 +35,22 @@ cudaError_t launch_chained(void (*kernel)(P...), unsigned grid, int threads, siz
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+// A positive number that depends on the current device, asked of `query` the first time on each (and every time on
+// ordinals that the table has no place for); 0 stands for not known yet.
+constexpr int kKnownDevices = 64;
+template <typename F>
+cudaError_t per_device(std::atomic<int> (&known)[kKnownDevices], int& value, F query) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const bool place = dev >= 0 && dev < kKnownDevices;
+  value = place ? known[dev].load(std::memory_order_acquire) : 0;
+  if (value > 0) return cudaSuccess;
+  e = query(value);
+  if (e == cudaSuccess && place) known[dev].store(value, std::memory_order_release);
+  return e;
+}
+
 // Sets a kernel's dynamic shared memory limit, the first time on every device (2 us of a small call).  `Kernel`
 // keeps one limit for all its launches.
 template <auto Kernel>

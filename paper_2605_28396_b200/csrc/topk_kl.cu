@@ -732,11 +732,11 @@ cudaError_t launch_plan(const TopkParams& p, int C, int64_t rows, int sm_count, 
   cudaError_t e = shared_limit<topk_kl_kernel<TIn, TOut, TH, CTAS>>(smem);
   if (e != cudaSuccess) return e;
   // as many clusters as the GPU holds at a time: their CTAs go on from row to row
-  static std::atomic<int> held[4];
+  static std::atomic<int> held[4][kKnownDevices];
   int log_c = 0;
   while ((1 << log_c) < C) ++log_c;
-  int n = C == 1 ? sm_count * CTAS : held[log_c].load();
-  if (n == 0) {
+  int n = sm_count * CTAS;
+  if (C > 1) e = per_device(held[log_c], n, [&](int& clusters) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(sm_count * CTAS / C * C));
     cfg.blockDim = dim3(TH + 64);
@@ -747,11 +747,10 @@ cudaError_t launch_plan(const TopkParams& p, int C, int64_t rows, int sm_count, 
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
-    if (e != cudaSuccess) return e;
-    if (n < 1) return cudaErrorInvalidConfiguration;
-    held[log_c].store(n);
-  }
+    const cudaError_t asked = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+    return asked == cudaSuccess && clusters < 1 ? cudaErrorInvalidConfiguration : asked;
+  });
+  if (e != cudaSuccess) return e;
   const int64_t clusters = n < rows ? n : rows;
   return launch_chained(kernel, (unsigned)(clusters * C), TH + 64, smem, C, s, p);
 }
