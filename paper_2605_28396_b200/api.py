@@ -688,6 +688,8 @@ def _matrix(name, t):
     if t.dim() < 2:
         raise ValueError(f"{name}: at least two dimensions")
     d, M, ld, first = t.shape[-1], 1, t.shape[-1], True
+    if 0 in t.shape[:-1]:   # no rows, whatever the strides
+        return 0, d, d
     for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
         if n != 1:
             if first:

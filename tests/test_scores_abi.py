@@ -159,3 +159,22 @@ def test_a_call_on_another_device_than_the_current_one(monkeypatch):
     api._call(torch.device("cuda:1"), fn, 7)
     api._call(torch.device("cuda:0"), fn, 8)
     assert seen == [(1, (7,)), (0, (8,))] and current == [0]
+
+
+@pytest.mark.parametrize("shape", [(0,), (2, 0), (0, 3), (0, 0), (2, 0, 3), (2, 0, 1)])
+def test_rows_of_which_there_are_none(monkeypatch, shape):
+    """An empty batch of any number of dimensions passes through the 8-bit operators."""
+    class Record:
+        def __getattr__(self, name):
+            return lambda *a: seen.append((name, a)) or 0
+    seen = []
+    monkeypatch.setattr(api, "_lib", Record())
+    monkeypatch.setattr(api, "_stream", lambda dev: 0)
+    q, scale = api.adwin_quantize_rows_i8(torch.zeros(*shape, 40))
+    assert q.shape == (*shape, 40) and scale.shape == shape
+    w, s5 = torch.zeros(5, 48, dtype=torch.int8)[:, :40], torch.zeros(5)
+    assert api.adwin_linear_i8(q, scale, w, s5).shape == (*shape, 5)
+    assert api.adwin_linear_i8(q, scale, w, s5, out=torch.zeros(*shape, 5)).shape == (*shape, 5)
+    (a, quant), (b, lin), _ = seen
+    assert a == "adwin_quantize_rows_i8" and quant[2:5] == (0, 40, 40) and quant[6] == 48
+    assert b == "adwin_linear_i8" and lin[1] == 48 and lin[4] == 48 and lin[6:9] == (0, 5, 40)
