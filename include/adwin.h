@@ -443,12 +443,12 @@ int adwin_token_logprobs(const void* logits, int dtype, int64_t B, int64_t T, in
                          void* cuda_stream);
 
 /*
- * Gradient of a loss of these scores with respect to the logits, for positions t < E_b:
+ * Gradient of a loss of logprob, entropy and top_logprobs with respect to the logits, for positions t < E_b:
  *   grad_k = d_logprob (1[k=y] - p_k) - d_entropy p_k (log p_k + entropy)
  *            + sum_j d_top_j (1[k=top_ids_j] - p_k),        p_k = exp(z_k - lse)
  * lse, entropy as adwin_token_logprobs returned them; d_logprob, d_entropy [B,T], d_top [B,T,K]
  * fp32: the loss's derivatives, each or NULL (= 0).  entropy may be NULL without d_entropy, top_ids
- * without d_top (then K is ignored).  `rest` carries no gradient.  Entries of top_ids may repeat one another and
+ * without d_top (then K is ignored).  lse and rest carry no gradient.  Entries of top_ids may repeat one another and
  * the token; -1 stands for none.  Other indices outside [0,V) are left out and raise
  * ADWIN_DEV_TOKEN_RANGE.  A row all of whose derivatives are 0 has the gradient 0, whatever its
  * logits, which are not read.  lse is an fp32 number: where it is of size 1e6 and more (nothing left

@@ -10,9 +10,10 @@
 // in tensor memory (exact: d < 2^17 keeps every sum below 2^31), operands by TMA in the 128-byte
 // swizzle, 128 entries of the contraction a k-block.  The pipeline is that of tc_pipeline.cuh: bytes
 // are laid out as for 64 bf16.  An accumulator becomes float(acc) * (step_x * step_w): three roundings.
-// The results leave through shared memory as whole pieces of rows: 4 096 x 2 560 against 151 936 channels 1.11 to 1.18 ms
-// (2.7 to 2.9 POP/s, then the power limit) where 16-byte stores of a lane's own row took 1.19 to 1.23; 777 x 1 000
-// against 50 257 channels (rows off 16-byte boundaries, fp32) 81 us, 294 with scattered 4-byte stores, 114 in pieces of 32.
+// The results leave through shared memory as whole pieces of rows: 4 096 x 2 560 against 151 936 channels 1.11 to 1.18 ms in a
+// captured graph on a cool GPU (2.7 to 2.9 POP/s), 1.22 to 1.27 in a series of calls at the power limit, where 16-byte stores of
+// a lane's own row took 1.19 to 1.23; 777 x 1 000 against 50 257 channels (rows off 16-byte boundaries, fp32) 81 to 88 us,
+// 294 with scattered 4-byte stores, 114 in pieces of 32.
 #include <cuda_bf16.h>
 
 #include "adwin_common.cuh"
@@ -437,7 +438,7 @@ cudaError_t launch_linear_i8(const int8_t* x, int64_t ldx, const float* step_x, 
                              const float* step_w, int64_t M, int64_t N, int64_t d, void* out, int out_dtype,
                              int64_t ldo, int32_t* status, int sm_count, cudaStream_t s) {
   // few tokens, d = 2 560 against 151 936 channels (389 MB: 59 us at the copy rate): 8 take 100 us on the tiles,
-  // 66 here, 16 98 and 75, 32 92 and 155
+  // 66 here, 16 98 and 75, 32 92 and 155; on the tiles 64 take 90, 128 97 and 256 107 (their rounding to 8 bits included)
   const int64_t row64 = (d + 63) / 64 * 64, pitch = row64 % 128 ? row64 : row64 + 64;
   const int tiles8 = (int)((M + 7) / 8);
   if (M <= kFewMax && tiles8 * 8 * pitch <= kFewSmemX) {

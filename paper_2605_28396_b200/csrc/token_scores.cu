@@ -1,5 +1,6 @@
 // Scores of given tokens under one policy: log probability, entropy, log-sum-exp, the K most likely
-// alternatives and the mass outside them; and the gradient of any loss of these scores.
+// alternatives and the mass outside them; and the gradient of a loss of the log probabilities and the entropy
+// (lse and the mass outside carry none).
 //
 // token_scores_kernel, one row (or a slice of it, see below) per CTA, read once:
 //   lse = M + ln S,  S = sum e^(z-M);   H = ln S + (sum e^(z-M) (M-z)) / S   (terms of one sign);
@@ -156,7 +157,8 @@ struct Units {
   static constexpr size_t kBytes = 10;   // per unit
 };
 // The CTA's shared memory.  The selection is not inlined (its registers would cost the sweep its own: 5 120 rows of
-// 151 936 entries 580 us inlined) and finds it by this name, not by a pointer that might lead anywhere.
+// 151 936 entries 580 us inlined; what lives across its call still spills at the 64 registers of eight CTAs per SM: 116 bytes
+// stored and 140 read back per thread, bf16) and finds it by this name, not by a pointer that might lead anywhere.
 extern __shared__ __align__(16) uint8_t score_smem[];
 template <int TH>
 __device__ __forceinline__ ScoreShared<TH>& score_shared() {
@@ -787,6 +789,7 @@ __global__ void __launch_bounds__(TH, TH == 128 ? 8 : 1) token_scores_kernel(con
         if (p.entropy) p.entropy[r] = finite ? fmaf(-tot.a / tot.s, kLn2, ln_s) : nan;
         if (p.lse) p.lse[r] = lse;
         if (TOP && p.rest)
+          // (beside a list of less than half the mass was summed for nothing: its share is known only with the list)
           p.rest[r] = !finite ? nan : listed < 0.5f ? log1pf(-listed) : (rest.m - tot.m) + (logf(rest.s) - ln_s);
         int bits = 0;
         if (!y_valid) bits |= ADWIN_DEV_TOKEN_RANGE;
@@ -935,7 +938,7 @@ __global__ void __launch_bounds__(TH, 1024 / TH) token_scores_bwd_kernel(const S
         }
         if (wide) {
           store_pairs<TOut>(out0 + (size_t)q * N * sizeof(TOut), g);
-        } else {
+        } else {   // an entry at a time (2 300 bf16 rows of 50 257, fp32 gradient: 150 us, 106 at the copy rate)
 #pragma unroll
           for (int j = 0; j < NP; ++j) {
             float a, b;
@@ -1002,7 +1005,12 @@ cudaError_t launch_token_scores(const void* logits, int dtype, int64_t B, int64_
   const int64_t rows = B * T;
   const bool bf = dtype == ADWIN_BF16;
   const int64_t pieces = V / (bf ? 8 : 4);
-  // few rows: clusters of CTAs with 512 threads share a row, so that the call reads with the whole GPU
+  // Few rows: clusters of two to eight CTAs with 512 threads share a row, as many as half of the SMs leave each.
+  // Many: a CTA of 128 threads each, eight per SM.  Calls between about 75 and 600 rows are the weak side of this rule:
+  // 75 rows keep half of the SMs idle.  151 936 bf16 entries, us without alternatives / with 20, read once at the
+  // copy rate in brackets: 8 rows 5.6 / 12.5 (0.4), 37 (four CTAs to a row) 14.7 / 30.2 (1.7), 38 (two) 10.4 / 17.5, 74 11.3 / 18.6 (3.4), 75 23.9 / 34.5 (3.5),
+  // 148 24.7 / 35.6 (6.9), 300 30.7 / 43.6 (13.9), 600 48.7 / 65.2 (27.8), 2 400 125 / 169 (111); fp32 74 12.8 / 20.7, 75
+  // 35.9 / 51.7, 600 62.4 / 82.2 (55.6), 2 400 227 / 286 (222).
   int C = 1;
   while (C < kMaxClusterX && rows * C * 2 <= sm_count && pieces >= (int64_t)C * 2 * 512) C *= 2;
   if (C > 1) {

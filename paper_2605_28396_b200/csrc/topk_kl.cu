@@ -644,7 +644,7 @@ struct TopkCta {
 #pragma unroll
         for (int x = 0; x < NP; ++x) g[x] = mul2(coef, ex2_2(mul2(add2(z[x], neg_m), splat2(kLog2e))));
       };
-      if (!wide) {   // rows of the gradient off its pieces' boundaries: an entry at a time
+      if (!wide) {   // rows of the gradient off its pieces' boundaries: an entry at a time (2 300 bf16 rows of 50 257, fp32: 172 us over 106)
 #pragma unroll 1
         for (int j = tid; j < np; j += TH) {
           f2_t g[NP];
@@ -763,12 +763,15 @@ cudaError_t launch(const TopkParams& p, int64_t rows, int sm_count, cudaStream_t
   while (C < kMaxCtas && rows * C * 2 <= sm_count && pieces >= (int64_t)C * 2 * 1024) C *= 2;
   // Many: as many threads to a row as leave each a few groups of pieces, about 32 warps per SM in all (bf16, us for 128
   // threads x 8 CTAs per SM / 256 x 4 / 512 x 2 / 960 x 1: 18 432 rows of 4 096 entries 225 / 369 / 552 / -,
-  // 2 560 of 32 000 139 / 129 / 136 / -, 2 300 of 50 257 116 / 104 / 107 / -, 5 120 of 151 936 - / - / 652 / 609;
+  // 2 560 of 32 000 139 / 129 / 136 / -, 2 300 of 50 257 116 / 104 / 107 / -, 5 120 of 151 936 - / - / 652 / 609 to 632;
   // the last with 512 x 2 in pairs 630, 256 x 4 in pairs 678)
   const bool few = rows * C <= sm_count;
   if (pieces / C < (few ? 1024 : 3000)) return launch_plan<TIn, TOut, 128, 8>(p, C, rows, sm_count, s);
   if (pieces / C < (few ? 4096 : 10000)) return launch_plan<TIn, TOut, 256, 4>(p, C, rows, sm_count, s);
-  // and not many more than 45 MB of rows at a time, or their second read misses L2
+  // The longest rows: not many more than 45 MB at a time, or their second read misses L2.  The plans above do not look
+  // at that: 592 rows at a time are 60 MB at 50 257 bf16 entries and 95 MB just below 80 000, and the reads from
+  // memory grow from 1.10 times the logits there over 1.31 (65 536) to 1.53 (2 300 rows: 104, 132, 171 us over 70, 92, 112 at
+  // the copy rate; fp32 rows of half as many entries 97, 126, 163).
   while (C < kMaxCtas && sm_count / C * p.V * (int64_t)sizeof(TIn) > (int64_t(50) << 20)) C *= 2;
   return launch_plan<TIn, TOut, 960, 1>(p, C, rows, sm_count, s);
 }
